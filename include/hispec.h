@@ -266,6 +266,75 @@ int ee_verify_level_rs(ee_session* s, int level, const uint8_t* active, const fl
  * verify call ee_debug_last_logits returns that call's target distributions instead of logits. */
 int ee_debug_read_dist(ee_session* s, int which, int seq, int row0, int n, float* host_out);
 
+/* ---- decoding rules ------------------------------------------------------------------------------
+ * What a caller asks of the next token besides the model's own preference, applied to a row's logits in this order, every step
+ * rounded to fp32 (c: how often the token stands in the history behind the prompt):
+ *   repetition  rho   tokens of the history, prompt included:  x > 0 ? x / rho : x * rho
+ *   frequency   f     x - f * c
+ *   presence    p     x - p   where c > 0
+ *   bias              x + bias(token); of a token that is listed twice the last entry counts
+ *   temperature T     x / T
+ *   allowed           -inf where the row's bit mask does not hold the token (bit t & 31 of word t >> 5)
+ *
+ * ee_logit_rules applies them to logits in device memory.  Rows belong to sequences: sequence b has the rows row_start[b] ..
+ * row_start[b+1]-1 and row i of it sees the first first_len[b]+i tokens of its history, as the rows of a verify block do; rows in front of row_start[0]
+ * and behind row_start[n_seq] are left alone.  Logits must not be NaN or +inf where allowed (masked ones may be anything).
+ * Token ids outside the vocabulary are ignored.  Nothing is allocated or synchronised; results do not vary from run to run. */
+typedef struct ee_rules_call {
+  int32_t n_seq, rows, vocab;
+  int32_t dtype;                 /* of the logits: EE_F32 or EE_BF16                                              */
+  const void* logits;            /* [rows][logits_stride]                                                         */
+  int64_t logits_stride;         /* elements, >= vocab                                                            */
+  float* out;                    /* [rows][out_stride]; may be `logits` itself (EE_F32, same stride)              */
+  int64_t out_stride;
+  int32_t probs;                 /* 0: the adjusted logits, 1: their softmax (all zero for a row that nothing may follow) */
+  int32_t n_bias;                /* entries of bias_token / bias_value                                            */
+  int32_t* argmax;               /* [rows] or null: highest adjusted logit, lowest id among equals; -1: none above -inf */
+  const int32_t* row_start;      /* [n_seq+1], not decreasing                                                     */
+  const int32_t* tokens;         /* [n_seq][tokens_stride] histories; null: no penalties                          */
+  int64_t tokens_stride;         /* entries from one history to the next, >= tokens_room                          */
+  const int32_t* first_len;      /* [n_seq] tokens that the first row sees                                        */
+  const int32_t* prompt_len;     /* [n_seq] leading tokens that are prompt; null: 0                               */
+  const float *repetition, *frequency, *presence, *temperature;      /* [n_seq] each; null: 1, 0, 0, 1.  repetition, temperature > 0 */
+  const int32_t* bias_start;     /* [n_seq+1] entries of sequence b; null: no biases                              */
+  const int32_t* bias_token;
+  const float* bias_value;
+  const uint32_t* allowed;       /* [allowed_rows][allowed_stride] bit masks; null: everything is allowed         */
+  int64_t allowed_stride;        /* words, >= ceil(vocab / 32)                                                    */
+  const int32_t* allowed_row;    /* [rows] mask of every row, outside 0..allowed_rows-1: no mask; null: mask r for row r */
+  int32_t allowed_rows;
+  int32_t tokens_room;           /* room of a history; tokens behind it are not counted                           */
+  void* workspace;               /* ee_logit_rules_bytes(rows, vocab) bytes, 256-byte aligned; not shared by calls that overlap in time */
+  size_t workspace_bytes;
+} ee_rules_call;
+size_t ee_logit_rules_bytes(int rows, int vocab);
+int ee_logit_rules(const ee_rules_call* call, void* stream);
+
+/* The same for the sequences of a session: every exit head -- drafting, verification at any exit, decoding, the first token behind a
+ * prompt, greedy and sampling calls alike -- then decides on the adjusted logits, row by row with the history of its position (C||V
+ * and the block's tokens in front of it), so that a greedy stream is still that of ee_decode_ar under the same rules.  Rolled-back
+ * tokens leave the history with their positions.
+ * ee_rules_attach: a caller-owned device arena of ee_rules_bytes(), 256-byte aligned, once per session; max_bias: room for biases per
+ * sequence.  ee_rules_set: the rules of one sequence's slot from now on, whatever prompt it holds (null: none); host memory, read
+ * before the call returns.  EE_ERR_ARG: repetition or temperature not positive, a number not finite, more than max_bias biases, a
+ * token outside the vocabulary, or masks that allow nothing.  Biases, penalties and 1 / temperature are limited to 1e6.
+ * ee_rules_rows: further masks for the next call that decides on tokens of the sequence (prompt, drafting, verification, decoding), mask j for
+ * its row or step j (a prompt has one row); rows behind them have the sequence's own mask only.  n <= max_rows; n == 0 and ee_rules_set take them
+ * back.  They serve one call that succeeds.  EE_ERR_STATE for a sequence without rules.
+ * The introspection calls report adjusted logits.  ee_verify_intermediate_static refuses (EE_ERR_STATE) while a sequence has rules. */
+typedef struct ee_rules {
+  float repetition, frequency, presence, temperature;    /* 1, 0, 0, 1: off */
+  int32_t n_bias;
+  int32_t reserved;                /* 0 */
+  const int32_t* bias_token;       /* host [n_bias] */
+  const float* bias_value;
+  const uint32_t* allowed;         /* host [ceil(vocab/32)] or null */
+} ee_rules;
+size_t ee_rules_bytes(const ee_session* s, int max_bias);
+int ee_rules_attach(ee_session* s, int max_bias, void* dev_arena, size_t arena_bytes);
+int ee_rules_set(ee_session* s, int seq, const ee_rules* rules);
+int ee_rules_rows(ee_session* s, int seq, int n, const uint32_t* allowed);   /* host [n][ceil(vocab/32)] */
+
 /* ---- introspection (parity tests; not part of the timed path) ---------------------------- */
 int ee_get_lengths(const ee_session* s, int32_t* len_by_batch);   /* host [batch, ee_n_levels()+1]: KV length of every layer group (3 for Alg. 2) */
 int ee_n_levels(const ee_session* s);   /* verifier exits after L_d: 2 (L_i, L_f) plus the model's extra exits */

@@ -15,11 +15,12 @@ from typing import Optional, Sequence, Tuple
 import numpy as np
 
 __all__ = [
-    "lib", "lib_path", "EEError", "ee_config", "make_config", "Model", "Session",
+    "lib", "lib_path", "EEError", "ee_config", "ee_rules_call", "ee_rules", "make_config", "Model", "Session", "LogitRules",
     "ee_model_bytes", "ee_model_load", "ee_model_set_tensor", "ee_model_get_tensor_rows", "ee_model_free",
     "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
     "ee_verify_intermediate", "ee_verify_intermediate_static", "ee_verify_full", "ee_verify_level", "ee_n_levels", "kv_rollback", "ee_sampling_bytes", "ee_sampling_attach",
-    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
+    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist",
+    "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
     "ee_debug_enable_logits", "ee_debug_last_logits", "ee_debug_last_hidden", "ee_debug_read_kv", "ee_debug_write_kv",
     "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
     "EE_F32", "EE_BF16", "TENSOR_IDS", "EXPORTED_SYMBOLS",
@@ -34,7 +35,8 @@ EXPORTED_SYMBOLS = [
     "ee_model_bytes", "ee_model_load", "ee_model_set_tensor", "ee_model_get_tensor_rows", "ee_model_free",
     "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
     "ee_verify_intermediate", "ee_verify_intermediate_static", "ee_verify_full", "ee_verify_level", "ee_n_levels", "kv_rollback", "ee_sampling_bytes", "ee_sampling_attach",
-    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
+    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist",
+    "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
     "ee_debug_enable_logits", "ee_debug_last_logits", "ee_debug_last_hidden", "ee_debug_read_kv", "ee_debug_write_kv",
     "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
 ]
@@ -46,6 +48,23 @@ class ee_config(C.Structure):
                [("rope_theta", C.c_float), ("rms_eps", C.c_float), ("dtype", C.c_int32),
                 ("bonus_inter", C.c_int32), ("bonus_full", C.c_int32), ("sigma", C.c_float), ("gamma", C.c_float * 3),
                 ("head_rank", C.c_int32), ("n_extra_exits", C.c_int32), ("extra_exits", C.c_int32 * 4)]
+
+
+class ee_rules_call(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("logits", C.c_void_p), ("logits_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64),
+                ("probs", C.c_int32), ("n_bias", C.c_int32), ("argmax", C.c_void_p), ("row_start", C.c_void_p),
+                ("tokens", C.c_void_p), ("tokens_stride", C.c_int64), ("first_len", C.c_void_p), ("prompt_len", C.c_void_p),
+                ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p), ("temperature", C.c_void_p),
+                ("bias_start", C.c_void_p), ("bias_token", C.c_void_p), ("bias_value", C.c_void_p),
+                ("allowed", C.c_void_p), ("allowed_stride", C.c_int64), ("allowed_row", C.c_void_p), ("allowed_rows", C.c_int32),
+                ("tokens_room", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class ee_rules(C.Structure):
+    _fields_ = [("repetition", C.c_float), ("frequency", C.c_float), ("presence", C.c_float), ("temperature", C.c_float),
+                ("n_bias", C.c_int32), ("reserved", C.c_int32), ("bias_token", C.POINTER(C.c_int32)),
+                ("bias_value", C.POINTER(C.c_float)), ("allowed", C.POINTER(C.c_uint32))]
 
 
 class EEError(RuntimeError):
@@ -97,6 +116,12 @@ def _load():
         "ee_verify_intermediate_rs": (C.c_int, [vp, f32p, C.c_int, f32p, i32p, i32p]),
         "ee_verify_full_rs": (C.c_int, [vp, C.POINTER(C.c_uint8), f32p, C.c_int, f32p, i32p, i32p, i32p, i32p]),
         "ee_verify_level_rs": (C.c_int, [vp, C.c_int, C.POINTER(C.c_uint8), f32p, C.c_int, f32p, i32p, i32p, i32p, i32p]),
+        "ee_logit_rules_bytes": (C.c_size_t, [C.c_int, C.c_int]),
+        "ee_logit_rules": (C.c_int, [C.POINTER(ee_rules_call), vp]),
+        "ee_rules_bytes": (C.c_size_t, [vp, C.c_int]),
+        "ee_rules_attach": (C.c_int, [vp, C.c_int, vp, C.c_size_t]),
+        "ee_rules_set": (C.c_int, [vp, C.c_int, C.POINTER(ee_rules)]),
+        "ee_rules_rows": (C.c_int, [vp, C.c_int, C.c_int, C.POINTER(C.c_uint32)]),
         "ee_get_lengths": (C.c_int, [vp, i32p]),
         "ee_get_counts": (C.c_int, [vp, i32p, i32p]),
         "ee_get_tokens": (C.c_int, [vp, C.c_int, i32p, C.c_int, i32p]),
@@ -364,6 +389,35 @@ def ee_verify_level_rs(session: int, level: int, batch: int, max_rows: int, u_ac
     _chk(lib.ee_verify_level_rs(session, level, act, _p_f32(u_acc), u_acc.shape[1], _p_f32(u_res), _p_i32(a), _p_i32(n),
                                 _p_i32(com), _p_i32(nc)))
     return a, n, [com[b, :nc[b]].tolist() for b in range(batch)]
+
+
+def ee_logit_rules_bytes(rows: int, vocab: int) -> int:
+    return int(lib.ee_logit_rules_bytes(rows, vocab))
+
+
+def ee_logit_rules(call: ee_rules_call, stream_ptr: int) -> None:
+    _chk(lib.ee_logit_rules(C.byref(call), stream_ptr))
+
+
+def ee_rules_bytes(session: int, max_bias: int) -> int:
+    n = lib.ee_rules_bytes(session, max_bias)
+    if n == 0:
+        raise EEError(-1, ee_last_error())
+    return int(n)
+
+
+def ee_rules_attach(session: int, max_bias: int, dev_ptr: int, nbytes: int) -> None:
+    _chk(lib.ee_rules_attach(session, max_bias, dev_ptr, nbytes))
+
+
+def ee_rules_set(session: int, seq: int, rules: Optional[ee_rules]) -> None:
+    _chk(lib.ee_rules_set(session, seq, C.byref(rules) if rules is not None else None))
+
+
+def ee_rules_rows(session: int, seq: int, allowed: np.ndarray) -> None:
+    m = np.ascontiguousarray(allowed, dtype=np.uint32)
+    assert m.ndim == 2
+    _chk(lib.ee_rules_rows(session, seq, m.shape[0], m.ctypes.data_as(C.POINTER(C.c_uint32))))
 
 
 def kv_rollback(session: int, seq: int, group_mask: int, new_len: int) -> None:
@@ -650,6 +704,40 @@ class Session:
     def verify_level_rs(self, level: int, u_acc: np.ndarray, u_res: np.ndarray, active=None):
         return ee_verify_level_rs(self.handle, level, self.batch, self.max_rows, u_acc, u_res, active)
 
+    def enable_rules(self, max_bias: int = 0) -> None:
+        """Allocate and attach the buffers of the decoding rules, with room for max_bias biases per sequence."""
+        n = ee_rules_bytes(self.handle, max_bias)
+        buf, ptr = _arena(n)
+        ee_rules_attach(self.handle, max_bias, ptr, n)
+        self._rules_buf = buf
+
+    def set_rules(self, seq: int, repetition: float = 1.0, frequency: float = 0.0, presence: float = 0.0, temperature: float = 1.0,
+                  bias: Optional[dict] = None, allowed=None) -> None:
+        """The decoding rules of a slot (enable_rules first).  bias: {token: number}; allowed: the tokens that may follow at all, as
+        truth values [vocab] or packed words [ceil(vocab / 32)]."""
+        r = ee_rules(repetition, frequency, presence, temperature)
+        tok, val = _i32(list((bias or {}).keys())), np.array(list((bias or {}).values()), np.float32)
+        r.n_bias, r.bias_token, r.bias_value = len(tok), _p_i32(tok), _p_f32(val)
+        if allowed is not None:
+            words = self._mask_words(np.asarray(allowed)[None])
+            r.allowed = words.ctypes.data_as(C.POINTER(C.c_uint32))
+        ee_rules_set(self.handle, seq, r)
+
+    def clear_rules(self, seq: int) -> None:
+        ee_rules_set(self.handle, seq, None)
+
+    def row_masks(self, seq: int, allowed) -> None:
+        """Masks of the rows (steps) of the next call that decides on tokens of the sequence: truth values [n, vocab] or packed words."""
+        ee_rules_rows(self.handle, seq, self._mask_words(np.asarray(allowed)))
+
+    def _mask_words(self, m: np.ndarray) -> np.ndarray:
+        words = (self.model.cfg.vocab + 31) // 32
+        if m.dtype == np.bool_ and m.ndim == 2 and m.shape[1] == self.model.cfg.vocab:
+            m = np.packbits(np.pad(m, ((0, 0), (0, words * 32 - m.shape[1]))), axis=1, bitorder="little").view("<u4")
+        if m.ndim != 2 or m.shape[1] != words or m.dtype.kind not in "ui" or m.dtype.itemsize != 4:
+            raise ValueError(f"masks are truth values of {self.model.cfg.vocab} tokens or {words} words of 32 bits a row")
+        return np.ascontiguousarray(m).view(np.uint32)
+
     def rollback(self, seq: int, group_mask: int, new_len: int) -> None:
         kv_rollback(self.handle, seq, group_mask, new_len)
 
@@ -701,3 +789,94 @@ class Session:
             self.close()
         except Exception:
             pass
+
+
+class LogitRules:
+    """Decoding rules for rows of logits in device memory (ee_logit_rules): holds the tensors that describe them and their addresses.
+
+    Arguments as the fields of ee_rules_call, tensors on one device: int32 row_start [n_seq+1], tokens [n_seq, room], first_len, prompt_len
+    [n_seq], bias_start [n_seq+1], bias_token, allowed_row [rows]; float32 repetition, frequency, presence, temperature [n_seq],
+    bias_value; int32 words allowed [masks, ceil(vocab / 32)].  Their contents may change between calls (a history that grows
+    in place).  Calls run on torch's current stream of that device."""
+
+    _KINDS = {"row_start": "i", "first_len": "i", "prompt_len": "i", "bias_start": "i", "bias_token": "i", "allowed_row": "i", "tokens": "i",
+              "allowed": "i", "repetition": "f", "frequency": "f", "presence": "f", "temperature": "f", "bias_value": "f"}
+
+    def __init__(self, vocab: int, row_start, *, tokens=None, first_len=None, prompt_len=None, repetition=None, frequency=None,
+                 presence=None, temperature=None, bias_start=None, bias_token=None, bias_value=None, allowed=None, allowed_row=None):
+        import torch
+        given = dict(row_start=row_start, tokens=tokens, first_len=first_len, prompt_len=prompt_len, repetition=repetition,
+                     frequency=frequency, presence=presence, temperature=temperature, bias_start=bias_start, bias_token=bias_token,
+                     bias_value=bias_value, allowed=allowed, allowed_row=allowed_row)
+        if not torch.is_tensor(row_start) or row_start.dim() != 1 or row_start.numel() < 1:
+            raise ValueError("row_start: an int32 tensor [n_seq + 1]")
+        self.device, self.n_seq, self.vocab = row_start.device, row_start.numel() - 1, int(vocab)
+        per_seq = {"first_len", "prompt_len", "repetition", "frequency", "presence", "temperature"}
+        c = self.call = ee_rules_call()
+        for name, t in given.items():
+            if t is None:
+                continue
+            want = torch.int32 if self._KINDS[name] == "i" else torch.float32
+            if not torch.is_tensor(t) or t.dtype != want or t.device != self.device:
+                raise ValueError(f"{name}: a {want} tensor on {self.device}")
+            two = name in ("tokens", "allowed")
+            if t.dim() != (2 if two else 1) or (t.numel() and t.stride(-1) != 1):
+                raise ValueError(f"{name}: {'two dimensions' if two else 'one dimension'}, its entries side by side")
+            if name in per_seq and t.numel() != self.n_seq or name == "bias_start" and t.numel() != self.n_seq + 1 or \
+                    name == "tokens" and t.shape[0] != self.n_seq:
+                raise ValueError(f"{name}: one entry for each of {self.n_seq} sequences")
+            setattr(c, name, t.data_ptr())
+        if tokens is not None:
+            c.tokens_room, c.tokens_stride = tokens.shape[1], max(tokens.stride(0), tokens.shape[1])
+        if allowed is not None:
+            c.allowed_rows = allowed.shape[0]
+            c.allowed_stride = allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]
+            if allowed.shape[1] < (self.vocab + 31) // 32:
+                raise ValueError("allowed: a bit for every token of the vocabulary")
+        if (bias_token is None) != (bias_value is None) or (bias_token is not None and bias_token.numel() != bias_value.numel()):
+            raise ValueError("bias_token and bias_value: as many entries")
+        c.n_bias = 0 if bias_token is None else bias_token.numel()
+        c.n_seq, c.vocab = self.n_seq, self.vocab
+        self._kept = given
+        self._rows = allowed_row.numel() if allowed_row is not None else None
+
+    def _run(self, x, probs: bool, argmax: bool, out):
+        import torch
+        if not torch.is_tensor(x) or x.dim() != 2 or x.shape[1] != self.vocab or x.device != self.device or \
+                x.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"logits: float32 or bfloat16 [rows, {self.vocab}] on {self.device}")
+        rows = x.shape[0]
+        if self._rows is not None and self._rows < rows:
+            raise ValueError(f"allowed_row: an entry for each of {rows} rows")
+        if self.vocab > 1 and x.stride(1) != 1:
+            raise ValueError("logits: the tokens of a row side by side")
+        if out is None:
+            out = torch.empty((rows, self.vocab), dtype=torch.float32, device=self.device)
+        elif not torch.is_tensor(out) or out.dtype != torch.float32 or out.shape != x.shape or out.device != self.device or \
+                (self.vocab > 1 and out.stride(1) != 1):
+            raise ValueError("out: float32 of the logits' shape, the tokens of a row side by side")
+        token = torch.empty(rows, dtype=torch.int32, device=self.device) if argmax else None
+        if rows == 0:
+            return (out, token) if argmax else out
+        work = torch.empty(ee_logit_rules_bytes(rows, self.vocab), dtype=torch.uint8, device=self.device)
+        c = ee_rules_call.from_buffer_copy(self.call)
+        c.rows, c.dtype, c.probs = rows, EE_F32 if x.dtype == torch.float32 else EE_BF16, int(probs)
+        c.logits, c.logits_stride = x.data_ptr(), x.stride(0) if rows > 1 else self.vocab
+        c.out, c.out_stride = out.data_ptr(), out.stride(0) if rows > 1 else self.vocab
+        c.argmax = token.data_ptr() if argmax else None
+        off = (-work.data_ptr()) % 256
+        c.workspace, c.workspace_bytes = work.data_ptr() + off, work.numel() - off
+        if torch.cuda.current_device() == self.device.index:
+            ee_logit_rules(c, torch.cuda.current_stream(self.device).cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                ee_logit_rules(c, torch.cuda.current_stream(self.device).cuda_stream)
+        return (out, token) if argmax else out
+
+    def logits(self, x, argmax: bool = False, out=None):
+        """The adjusted logits (float32); with argmax also the token of every row (int32, -1 where nothing may follow)."""
+        return self._run(x, False, argmax, out)
+
+    def probs(self, x, argmax: bool = False, out=None):
+        """Their softmax (float32); a row that nothing may follow is all zeros."""
+        return self._run(x, True, argmax, out)

@@ -135,3 +135,12 @@ void k_rs_accept(hipStream_t st, const float* Pt, const float* Pd, int pd_rows_p
                  int cand_stride, int B, const float* u_acc, int u_stride, int* n_accept);
 void k_rs_draw(hipStream_t st, const float* Pt, const float* Pd, int pd_rows_per_seq, int vocab, const CallMeta& meta, int B,
                const int* n_accept, const float* u_res, int* result);   // result: n_accept [B], then the drawn tokens [B]
+
+// ---- decoding rules (kernels_rules.hip) ----
+// One step of a sequential pass (drafting, decoding): first_len counts `add` tokens more, the last of which (last[first row of the sequence])
+// is not in the list yet and is stored into hist; allowed_row advances by whole calls of rows; take: as for the arg max kernels.
+struct RulesStep { int add = 0; const int* last = nullptr; int* hist = nullptr; TakeToken take; };
+size_t k_rules_workspace(int rows, int vocab);
+void k_rules(hipStream_t st, const ee_rules_call& call, const RulesStep& step);
+// dev[0..n) <- host (page-locked); token lists: list b of dst (stride entries) gets entries [delta[2b], delta[2b] + delta[2b+1]) of list b of src
+void k_rules_upload(hipStream_t st, const int* host, int* dev, int n, const int* src, int* dst, const int* delta, size_t stride, int B);

@@ -17,6 +17,7 @@ struct SeqState {
   int n_hd = 0;               // buffered L_d hidden rows (pending draft block incl. bonus row)
   int n_pi = 0;               // rejection sampling: tokens of V whose L_i distribution is stored
   int n_pu[4] = {0, 0, 0, 0}; // ... and tokens of the buffers at the further verifier exits (levels 2..n-1) whose distribution is stored
+  int n_prompt = 0;           // leading tokens of C that the prompt brought (rules count presence and frequency behind them)
   bool sampled = false;       // the pending draft block was drawn from p_{L_d} (its distributions are stored)
   std::vector<int> pages;     // block table
   bool started = false;
@@ -30,6 +31,32 @@ struct MetaSlot {             // one upload region: host (pinned) + device copy,
 };
 
 struct KTimer { int fam; hipEvent_t a, b; };
+
+// Decoding rules of a session (ee_rules_*): the rules of every slot, and what lies in the attached arena.
+struct RuleSlot {
+  bool on = false;
+  std::vector<uint32_t> allowed;   // the sequence's own mask (empty: none)
+  int n_rows = 0;                  // masks of its next call's rows
+};
+struct SessionRules {
+  std::vector<RuleSlot> slot;
+  int max_bias = 0, words = 0, n_on = 0;
+  // device: token lists [B][max_ctx], parameters [4][B] (repetition, frequency, presence, temperature), biases [B][max_bias] (unused entries: token -1),
+  // masks [B][1 + max_rows][words] (the sequence's own, then those of rows), the kernels' workspace, the tables of a call
+  int *hist = nullptr, *bias_start = nullptr, *bias_token = nullptr, *table = nullptr;
+  float *param = nullptr, *bias_value = nullptr;
+  uint32_t* mask = nullptr;
+  void* work = nullptr;
+  size_t work_bytes = 0;
+  // page-locked host: the token lists (the first known[b] entries of list b are in `hist` as well), the tables of a call
+  int *h_hist = nullptr, *h_table = nullptr;
+  std::vector<int> known;
+  hipEvent_t uploaded = nullptr;
+  // offsets in the tables: row_start [B+1], first_len [B], prompt_len [B], delta [B][2], allowed_row [rows or steps * rows]
+  size_t o_first = 0, o_prompt = 0, o_delta = 0, o_allowed = 0, ints = 0;
+  // the call at hand: rows of a pass; 0: no rules apply
+  int rows = 0;
+};
 
 struct ee_session {
   ee_model* m = nullptr;
@@ -55,6 +82,7 @@ struct ee_session {
   float *Pd = nullptr, *Pi = nullptr;
   float* Pup[4] = {nullptr, nullptr, nullptr, nullptr};   // the same for the buffers of levels 2..n-1
   bool need_logits = false;
+  SessionRules rules;
   float *part_o = nullptr, *part_ml = nullptr, *pmax = nullptr, *ssq = nullptr, *gemm_part = nullptr, *inv_rms = nullptr;
   // auxiliary exit heads: adapter output rows z [maxM][d], its rank-r intermediate (T: fp32 models, the rows; TF: bf16
   // models, the operand of the up projection), that operand's unused sum-of-squares partials, unit gains
@@ -244,6 +272,9 @@ extern "C" void ee_session_free(ee_session* s) {
     if (s->slot[i].copied) (void)hipEventDestroy(s->slot[i].copied);
   }
   if (s->out_host) (void)hipHostFree(s->out_host);
+  if (s->rules.h_hist) (void)hipHostFree(s->rules.h_hist);
+  if (s->rules.h_table) (void)hipHostFree(s->rules.h_table);
+  if (s->rules.uploaded) (void)hipEventDestroy(s->rules.uploaded);
   delete s;
 }
 
@@ -453,6 +484,83 @@ static void reset_accounting(ee_session* s) {
 }
 
 // ---------------------------------------------------------------------------------------------
+// decoding rules of a call
+// ---------------------------------------------------------------------------------------------
+// m[b] rows of sequence b behind first_len[b] - 1 tokens each, packed in sequence order; text(b): the tokens that its rows may see; masked(b, row):
+// the number of the row's (or its step's) own mask, or -1.  steps > 1: a sequential pass of so many steps of one row each.
+template <class TextFn, class MaskFn>
+static int rules_begin(ee_session* s, const std::vector<int>& m, const std::vector<int>& first_len, int steps, TextFn text, MaskFn masked) {
+  SessionRules& R = s->rules;
+  R.rows = 0;
+  if (!R.n_on) return EE_OK;
+  HIP_TRY(hipEventSynchronize(R.uploaded));              // (the tables of an earlier pass of this call are on the device)
+  int* h = R.h_table;
+  int row = 0;
+  for (int b = 0; b < s->B; ++b) {
+    const RuleSlot& q = R.slot[b];
+    h[b] = row; h[R.o_first + b] = 0; h[R.o_prompt + b] = s->seq[b].n_prompt;
+    h[R.o_delta + 2 * b] = h[R.o_delta + 2 * b + 1] = 0;
+    row += m[b];
+    if (!m[b] || !q.on) continue;
+    h[R.o_first + b] = first_len[b];
+    int* list = R.h_hist + (size_t)b * s->max_ctx;
+    const int known = R.known[b];
+    int n = 0;
+    text(b, [&](const int* t, size_t cnt) {              // (pieces of the text one after the other; what the list holds is passed over)
+      const int end = std::min<size_t>(n + cnt, s->max_ctx), from = std::max(n, known);
+      if (from < end) std::copy(t + (from - n), t + (end - n), list + from);
+      n = end;
+    });
+    h[R.o_delta + 2 * b] = std::min(known, n); h[R.o_delta + 2 * b + 1] = std::max(0, n - known);
+    R.known[b] = std::min(n, std::max(known, s->seq[b].cut[s->n_levels]));   // (committed tokens stay; the others may change until the next call)
+  }
+  h[s->B] = row;
+  for (int j = 0; j < steps; ++j)
+    for (int b = 0, r = 0; b < s->B; ++b)
+      for (int i = 0; i < m[b]; ++i, ++r) {
+        const RuleSlot& q = R.slot[b];
+        const int k = masked(b, steps > 1 ? j : i);
+        h[R.o_allowed + (size_t)j * row + r] = k >= 0 && k < q.n_rows ? b * (s->max_rows + 1) + 1 + k
+                                               : q.on && !q.allowed.empty() ? b * (s->max_rows + 1) : -1;
+      }
+  k_rules_upload(s->st, h, R.table, (int)(R.o_allowed + (size_t)steps * row), R.h_hist, R.hist, h + R.o_delta, s->max_ctx, s->B);
+  HIP_TRY(hipEventRecord(R.uploaded, s->st));
+  R.rows = row;
+  return EE_OK;
+}
+// tokens of a sequence from position n on may change
+static void forget_tokens(ee_session* s, int b, int n) {
+  if (!s->rules.known.empty()) s->rules.known[b] = std::min(s->rules.known[b], n);
+}
+// the rules on rows 0..M-1 of LOGITS, in place, and their arg max -> vtok
+static void apply_rules(ee_session* s, int M, const RulesStep& step) {
+  const SessionRules& R = s->rules;
+  ee_rules_call c;
+  memset(&c, 0, sizeof(c));
+  c.n_seq = s->B; c.rows = M; c.vocab = s->m->cfg.vocab; c.dtype = EE_F32;
+  c.logits = c.out = s->LOGITS; c.logits_stride = c.out_stride = c.vocab;
+  c.argmax = s->vtok;
+  c.row_start = R.table;
+  c.tokens = R.hist; c.tokens_stride = c.tokens_room = s->max_ctx; c.first_len = R.table + R.o_first; c.prompt_len = R.table + R.o_prompt;
+  c.repetition = R.param; c.frequency = R.param + s->B; c.presence = R.param + 2 * s->B; c.temperature = R.param + 3 * s->B;
+  if (R.max_bias > 0) { c.n_bias = s->B * R.max_bias; c.bias_start = R.bias_start; c.bias_token = R.bias_token; c.bias_value = R.bias_value; }
+  c.allowed = R.mask; c.allowed_stride = R.words; c.allowed_row = R.table + R.o_allowed; c.allowed_rows = s->B * (s->max_rows + 1);
+  c.workspace = R.work; c.workspace_bytes = R.work_bytes;
+  k_rules(s->st, c, step);
+}
+// a call that used the rules is over: masks of rows served it; device[b]: the lists' entries from there on were stored by the device
+static void rules_end(ee_session* s, const std::vector<int>& m, const std::vector<int>* device = nullptr) {
+  SessionRules& R = s->rules;
+  R.rows = 0;
+  if (R.slot.empty()) return;
+  for (int b = 0; b < s->B; ++b) {
+    if (!m[b]) continue;
+    R.slot[b].n_rows = 0;
+    if (device) R.known[b] = std::min(R.known[b], R.slot[b].on ? (*device)[b] : 0);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
 // forward pass pieces
 // ---------------------------------------------------------------------------------------------
 // the skinny kernel for few rows (see strips_serve), the row-tiled one up to 512 (wide matrices: 256), beyond the blocked one or the row-tiled one
@@ -588,13 +696,18 @@ static void run_layers(ee_session* s, int l0, int l1, const CallPlan& p, const C
 // row0 (a multiple of 16): the rows are row0 .. row0+M-1 of the pass instead (final exit only).  ended: the rows are those
 // listed on the device (the ends of prompts in a context build), normalised here; X's other rows need no head.
 // take: hand every row's token on (drafting, decoding).
-static void exit_head(ee_session* s, int M, int which, int row0 = 0, const int* ended = nullptr, const TakeToken& take = TakeToken()) {
+// step: of a sequential pass under rules (j > 0: the token that the step before took is tok_next).
+static void exit_head(ee_session* s, int M, int which, int row0 = 0, const int* ended = nullptr, const TakeToken& take = TakeToken(), int step = 0) {
   const ee_model* m = s->m;
   const ee_config& c = m->cfg;
   hipStream_t st = s->st;
   const int d = c.d_model, r = c.head_rank;
   const float* gf = (const float*)(m->base + m->gfinal);
   const bool aux = r > 0 && which < s->n_levels;
+  const bool rules = s->rules.rows > 0;
+  RulesStep rs;
+  if (step > 0) { rs.add = step; rs.last = s->tok_next; rs.hist = s->rules.hist; }
+  rs.take = take;
   if (m->bf16) {
     // the last down projection of the pass left XN = bf16(x * gain) and the partial sums of squares
     const int Mp = s->ssq_stride;
@@ -622,9 +735,10 @@ static void exit_head(ee_session* s, int M, int which, int row0 = 0, const int* 
     // (max, arg max) partials [row][tile]: the reduction of a row then reads one contiguous strip
     const int pstride = m->head.ntiles();
     o.pmax = s->pmax; o.pidx = s->pidx; o.pstride = pstride;
-    if (s->debug_logits || s->need_logits) { o.Y = s->LOGITS; o.ldy = c.vocab; }
+    if (s->debug_logits || s->need_logits || rules) { o.Y = s->LOGITS; o.ldy = c.vocab; }
     KF(KF_GEMM_HEAD, gemm(s, EPI_ARGMAX, m->head, operand, M, o));
-    KF(KF_ARGMAX, bf16_argmax_reduce(st, s->pmax, s->pidx, m->head.ntiles(), pstride, M, s->vtok, take));
+    if (rules) KF(KF_ARGMAX, apply_rules(s, M, rs));
+    else KF(KF_ARGMAX, bf16_argmax_reduce(st, s->pmax, s->pidx, m->head.ntiles(), pstride, M, s->vtok, take));
   } else {
     const float* hidden = s->X;
     if (aux) {
@@ -635,7 +749,8 @@ static void exit_head(ee_session* s, int M, int which, int row0 = 0, const int* 
       hidden = s->Z;
     }
     KF(KF_GEMM_HEAD, f32_gemm(st, hidden, d, gf, c.rms_eps, (const float*)(m->base + m->head.off), s->LOGITS, c.vocab, M, c.vocab, d, false));
-    KF(KF_ARGMAX, f32_argmax(st, s->LOGITS, M, c.vocab, s->vtok, take));
+    if (rules) KF(KF_ARGMAX, apply_rules(s, M, rs));
+    else KF(KF_ARGMAX, f32_argmax(st, s->LOGITS, M, c.vocab, s->vtok, take));
   }
   s->last_rows = M; s->last_row0 = row0;
 }
@@ -679,6 +794,8 @@ static int prefill_impl(ee_session* s, const int32_t* tokens, const int32_t* len
     SeqState& q = s->seq[b];
     for (int pg : q.pages) s->free_pages.push_back(pg);
     q = SeqState();
+    q.n_prompt = lens[b];
+    forget_tokens(s, b, 0);
   }
   reset_accounting(s);
   std::vector<size_t> off0(s->B, 0);
@@ -738,21 +855,39 @@ static int prefill_impl(ee_session* s, const int32_t* tokens, const int32_t* len
     CallMeta mt = meta_ptrs(s, s->slot[si].d);
     PassSource from_tokens; from_tokens.tok = mt.row_tok;
     run_layers(s, 0, c.n_layers, p, mt, 0, from_tokens, PassSink(), tail.on ? &tail : nullptr);
+    // the rules of a head over rows[b] rows per sequence, the first behind seen[b] - 1 tokens; a prompt's last row takes its mask 0
+    auto rules = [&](const std::vector<int>& rows, const std::vector<int>& seen) {
+      return rules_begin(s, rows, seen, 1, [&](int b, auto add) { add(tokens + off0[b], (size_t)lens[b]); },
+                         [&](int b, int i) { return seen[b] + i == lens[b] ? 0 : -1; });
+    };
     if (bf && n_end) {
       const bool kept_piece = s->debug_logits && last_pass;
       int early = 0;                                     // ends in front of that piece (all of them where it gets no head)
       while (early < n_end && !(kept_piece && end_row[early] >= r0)) ++early;
       if (early) {
+        std::vector<int> rows(s->B, 0), seen(s->B, 0);
+        for (int e = 0; e < early; ++e) { rows[end_seq[e]] = 1; seen[end_seq[e]] = lens[end_seq[e]]; }
+        EE_TRY(rules(rows, seen));
         exit_head(s, early, s->n_levels, 0, mt.row_src);
         HIP_TRY(hipMemcpyAsync(s->out_host + n_first, s->vtok, early * sizeof(int), hipMemcpyDeviceToHost, s->st));
       }
       if (kept_piece) {
+        std::vector<int> rows(s->B, 0), seen(s->B, 0);
+        for (int b = 0, first = 0; b < s->B; first += p.m[b], ++b) {
+          const int skip = std::max(0, piece0 - first);
+          if (skip >= p.m[b]) continue;
+          rows[b] = p.m[b] - skip; seen[b] = p.p0[b] + skip + 1;
+        }
+        EE_TRY(rules(rows, seen));
         exit_head(s, piece_rows, s->n_levels, r0);
         for (int e = early; e < n_end; ++e)
           HIP_TRY(hipMemcpyAsync(s->out_host + n_first + e, s->vtok + (end_row[e] - r0), sizeof(int), hipMemcpyDeviceToHost, s->st));
       }
       s->last_rows = piece_rows; s->last_row0 = r0;
     } else if (n_end) {
+      std::vector<int> seen(s->B);
+      for (int b = 0; b < s->B; ++b) seen[b] = p.p0[b] + 1;
+      EE_TRY(rules(p.m, seen));
       exit_head(s, p.M, s->n_levels);
       for (int e = 0; e < n_end; ++e)
         HIP_TRY(hipMemcpyAsync(s->out_host + n_first + e, s->vtok + end_row[e], sizeof(int), hipMemcpyDeviceToHost, s->st));
@@ -763,10 +898,13 @@ static int prefill_impl(ee_session* s, const int32_t* tokens, const int32_t* len
   }
   size_t off = 0;
   EE_TRY(finish(s));
+  rules_end(s, std::vector<int>(lens, lens + s->B));
   off = 0;
   for (int b = 0; b < s->B; ++b) {
     if (lens[b] <= 0) continue;
     SeqState& q = s->seq[b];
+    if (s->rules.n_on && s->rules.slot[b].on) s->rules.known[b] = lens[b];
+    q.n_prompt = lens[b];
     q.C.assign(tokens + off, tokens + off + lens[b]);
     q.C.push_back(s->out_host[first_slot[b]]);
     settle(s, q);
@@ -802,6 +940,7 @@ extern "C" int ee_seq_release(ee_session* s, int seq) {
   SeqState& q = s->seq[seq];
   while (!q.pages.empty()) { s->free_pages.push_back(q.pages.back()); q.pages.pop_back(); }
   q = SeqState();
+  forget_tokens(s, seq, 0);
   return EE_OK;
 }
 
@@ -834,13 +973,17 @@ extern "C" int ee_decode_ar(ee_session* s, int n, int32_t* out) {
   EE_TRY(build_meta(s, 0, p, [&](int b, int, int& tok, int&, int&) { tok = s->seq[b].C.back(); }));
   EE_TRY(upload_meta(s, 0));
   CallMeta mt = meta_ptrs(s, s->slot[0].d);
+  std::vector<int> seen(s->B);
+  for (int b = 0; b < s->B; ++b) seen[b] = p.p0[b] + 1;
+  EE_TRY(rules_begin(s, p.m, seen, n, [&](int b, auto add) { add(s->seq[b].C.data(), s->seq[b].C.size()); }, [](int, int j) { return j; }));
   int* dh = s->out_host + 2 * s->B;   // (pinned: the kernels store the tokens there)
   for (int j = 0; j < n; ++j) {       // the next token stays on the device; positions advance through pos_add
     PassSource from_tokens; from_tokens.tok = j == 0 ? mt.row_tok : s->tok_next;
     run_layers(s, 0, c.n_layers, p, mt, j, from_tokens);
-    exit_head(s, p.M, s->n_levels, 0, nullptr, TakeToken{s->tok_next, dh, mt.row_seq, s->max_rows, j});
+    exit_head(s, p.M, s->n_levels, 0, nullptr, TakeToken{s->tok_next, dh, mt.row_seq, s->max_rows, j}, j);
   }
   EE_TRY(finish(s));
+  rules_end(s, p.m, &seen);
   for (int b = 0; b < s->B; ++b) {
     SeqState& q = s->seq[b];
     if (!p.m[b]) { for (int j = 0; j < n; ++j) out[b * n + j] = -1; continue; }
@@ -916,13 +1059,19 @@ static int draft_impl(ee_session* s, int k, int32_t* draft, const float* u) {
   if (u) put_uniforms(s, p, u, k, nullptr);
   EE_TRY(upload_meta(s, 0));
   CallMeta mt = meta_ptrs(s, s->slot[0].d);
+  std::vector<int> seen(s->B);
+  for (int b = 0; b < s->B; ++b) seen[b] = p.p0[b] + 1;
+  EE_TRY(rules_begin(s, p.m, seen, k, [&](int b, auto add) {
+    add(s->seq[b].C.data(), s->seq[b].C.size());
+    add(s->seq[b].V.data(), s->seq[b].V.size());
+  }, [](int, int j) { return j; }));
   int* dh = s->out_host + 2 * s->B;   // (pinned: the kernels store the tokens there)
   for (int j = 0; j < rows; ++j) {
     PassSource from_tokens; from_tokens.tok = j == 0 ? mt.row_tok : s->tok_next;
     PassSink keep; keep.rows = s->Hd; keep.row_idx = mt.row_dst; keep.add = j;
     run_layers(s, 0, c.exit_draft, p, mt, j, from_tokens, keep);
     if (j < k) {
-      exit_head(s, p.M, 0, 0, nullptr, u ? TakeToken() : TakeToken{s->tok_next, dh, mt.row_seq, s->max_rows, j});
+      exit_head(s, p.M, 0, 0, nullptr, u ? TakeToken() : TakeToken{s->tok_next, dh, mt.row_seq, s->max_rows, j}, j);
       if (u)      // p_{L_d} of this position into the draft-distribution store, then the draw
         KF(KF_MISC, k_softmax_draw(s->st, s->LOGITS, s->Pd, mt.row_dst, j, p.M, c.vocab, uniforms(s), s->max_rows, j, mt.row_seq, s->tok_next,
                                    dh, s->max_rows));
@@ -930,6 +1079,7 @@ static int draft_impl(ee_session* s, int k, int32_t* draft, const float* u) {
   }
   s->need_logits = false;
   EE_TRY(finish(s));
+  rules_end(s, p.m, &seen);
   for (int b = 0; b < s->B; ++b) {
     SeqState& q = s->seq[b];
     if (!p.m[b]) { for (int j = 0; j < k; ++j) draft[b * k + j] = -1; continue; }
@@ -1120,6 +1270,12 @@ static int verify_intermediate_impl(ee_session* s, int32_t* n_accept, int32_t* n
   CallMeta mt = meta_ptrs(s, s->slot[0].d);
   PassSource kept; kept.rows = s->Hd; kept.row_idx = mt.row_src;       // a1: consume buffered H_d
   PassSink keep; keep.rows = s->Hi; keep.row_idx = mt.row_dst;          // keep L_i hidden rows
+  std::vector<int> seen(s->B);
+  for (int b = 0; b < s->B; ++b) seen[b] = p.p0[b] + 1;
+  EE_TRY(rules_begin(s, p.m, seen, 1, [&](int b, auto add) {
+    const SeqState& q = s->seq[b];
+    add(q.C.data(), q.C.size()); add(q.V.data(), q.V.size()); add(q.S.data(), q.S.size());
+  }, [](int, int i) { return i; }));
   run_layers(s, c.exit_draft, c.exit_inter, p, mt, 0, kept, keep);
   s->need_logits = rs;
   exit_head(s, p.M, 1);
@@ -1134,6 +1290,7 @@ static int verify_intermediate_impl(ee_session* s, int32_t* n_accept, int32_t* n
     KF(KF_ACCEPT, k_accept(s->st, s->vtok, mt, s->cand_stride, s->B, s->out_host, s->out_host + s->B));
   }
   EE_TRY(finish(s));
+  rules_end(s, p.m);
   for (int b = 0; b < s->B; ++b) {
     SeqState& q = s->seq[b];
     n_accept[b] = s->out_host[b]; next_token[b] = s->out_host[s->B + b];
@@ -1156,6 +1313,7 @@ extern "C" int ee_verify_intermediate(ee_session* s, int32_t* n_accept, int32_t*
 
 extern "C" int ee_verify_intermediate_static(ee_session* s, int32_t* n_accept, int32_t* next_token) {
   if (s && s->time_kernels) { ee_set_error("kernel timing creates events: switch it off for the call that allocates nothing"); return EE_ERR_STATE; }
+  if (s && s->rules.n_on) { ee_set_error("sequences have decoding rules, whose scratch is not in the static array: use ee_verify_intermediate"); return EE_ERR_STATE; }
   return verify_intermediate_impl(s, n_accept, next_token, nullptr, 0, nullptr, true);
 }
 
@@ -1269,6 +1427,10 @@ static int verify_upper_impl(ee_session* s, int level, const uint8_t* active, in
   PassSource kept; kept.rows = rows_below; kept.row_idx = mt.row_src;  // consume the buffered rows
   PassSink keep;
   if (j < n) { keep.rows = level_rows(s, j); keep.row_idx = mt.row_dst; }   // keep exit j's rows
+  EE_TRY(rules_begin(s, p.m, base, 1, [&](int b, auto add) {
+    add(s->seq[b].C.data(), s->seq[b].C.size());
+    add(s->seq[b].V.data(), s->seq[b].V.size());
+  }, [](int, int i) { return i; }));
   run_layers(s, ex[j - 1], ex[j], p, mt, 0, kept, keep);
   s->need_logits = rs;
   exit_head(s, p.M, j);
@@ -1284,6 +1446,7 @@ static int verify_upper_impl(ee_session* s, int level, const uint8_t* active, in
     KF(KF_ACCEPT, k_accept(s->st, s->vtok, mt, s->cand_stride, s->B, s->out_host, s->out_host + s->B));
   }
   EE_TRY(finish(s));
+  rules_end(s, p.m);
   for (int b = 0; b < s->B; ++b) {
     SeqState& q = s->seq[b];
     n_accept[b] = s->out_host[b]; next_token[b] = s->out_host[s->B + b];
@@ -1354,6 +1517,137 @@ extern "C" int ee_sampling_attach(ee_session* s, void* dev_arena, size_t arena_b
 }
 
 // ---------------------------------------------------------------------------------------------
+// C ABI: decoding rules (caller-owned arena, like the sampling buffers)
+// ---------------------------------------------------------------------------------------------
+static size_t carve_rules(const ee_session* s, int max_bias, char* base, SessionRules& R) {
+  const size_t B = s->B, vocab = s->m->cfg.vocab;
+  R.max_bias = max_bias;
+  R.words = (int)((vocab + 31) / 32);
+  R.o_first = B + 1; R.o_prompt = R.o_first + B; R.o_delta = R.o_prompt + B; R.o_allowed = R.o_delta + 2 * B;
+  R.ints = R.o_allowed + s->headM;                             // (headM >= batch * max_rows: verify rows, or steps of one row each)
+  Carver cv{base};
+  R.hist = cv.take<int>(B * s->max_ctx);
+  R.param = cv.take<float>(4 * B);
+  R.bias_start = cv.take<int>(B + 1);
+  R.bias_token = cv.take<int>(B * max_bias);
+  R.bias_value = cv.take<float>(B * max_bias);
+  R.mask = cv.take<uint32_t>(B * (s->max_rows + 1) * R.words);
+  R.table = cv.take<int>(R.ints);
+  R.work_bytes = k_rules_workspace(s->headM, (int)vocab);
+  R.work = cv.take<char>(R.work_bytes);
+  return align_up(cv.cur, 256);
+}
+extern "C" size_t ee_rules_bytes(const ee_session* s, int max_bias) {
+  if (!s || max_bias < 0 || max_bias > s->m->cfg.vocab) { ee_set_error("bad session or number of biases"); return 0; }
+  SessionRules R;
+  return carve_rules(s, max_bias, nullptr, R);
+}
+
+extern "C" int ee_rules_attach(ee_session* s, int max_bias, void* dev_arena, size_t arena_bytes) {
+  if (!s || !dev_arena || ((uintptr_t)dev_arena & 255)) { ee_set_error("arena must be non-null and 256-byte aligned"); return EE_ERR_ARG; }
+  if (max_bias < 0 || max_bias > s->m->cfg.vocab) { ee_set_error("bad number of biases"); return EE_ERR_ARG; }
+  if (s->rules.h_hist) { ee_set_error("rules are attached already"); return EE_ERR_STATE; }
+  SessionRules R;
+  if (arena_bytes < carve_rules(s, max_bias, (char*)dev_arena, R)) { ee_set_error("rules arena too small"); return EE_ERR_ARG; }
+  R.slot.resize(s->B); R.known.assign(s->B, 0);
+  std::vector<float> param(4 * (size_t)s->B, 0.f);
+  for (int b = 0; b < s->B; ++b) param[b] = param[3 * (size_t)s->B + b] = 1.f;
+  std::vector<int> start(s->B + 1), none((size_t)s->B * max_bias, -1);
+  for (int b = 0; b <= s->B; ++b) start[b] = b * max_bias;
+  hipError_t e = hipHostMalloc((void**)&R.h_hist, (size_t)s->B * s->max_ctx * sizeof(int), hipHostMallocDefault);
+  if (e == hipSuccess) e = hipHostMalloc((void**)&R.h_table, R.ints * sizeof(int), hipHostMallocDefault);
+  if (e == hipSuccess) e = hipEventCreateWithFlags(&R.uploaded, hipEventDisableTiming);
+  if (e == hipSuccess) e = hipMemcpyAsync(R.param, param.data(), param.size() * sizeof(float), hipMemcpyHostToDevice, s->st);
+  if (e == hipSuccess) e = hipMemcpyAsync(R.bias_start, start.data(), start.size() * sizeof(int), hipMemcpyHostToDevice, s->st);
+  if (e == hipSuccess && max_bias) e = hipMemcpyAsync(R.bias_token, none.data(), none.size() * sizeof(int), hipMemcpyHostToDevice, s->st);
+  if (e == hipSuccess) e = hipStreamSynchronize(s->st);
+  if (e != hipSuccess) {
+    if (R.h_hist) (void)hipHostFree(R.h_hist);
+    if (R.h_table) (void)hipHostFree(R.h_table);
+    if (R.uploaded) (void)hipEventDestroy(R.uploaded);
+    ee_set_error("rules attach: %s", hipGetErrorString(e));
+    return EE_ERR_HIP;
+  }
+  s->rules = R;
+  return EE_OK;
+}
+
+// a mask with the bits behind the vocabulary cleared; false: it allows nothing
+static bool tidy_mask(uint32_t* m, int words, int vocab) {
+  if (vocab & 31) m[words - 1] &= (1u << (vocab & 31)) - 1;
+  for (int w = 0; w < words; ++w)
+    if (m[w]) return true;
+  return false;
+}
+
+extern "C" int ee_rules_set(ee_session* s, int seq, const ee_rules* r) {
+  if (!s || seq < 0 || seq >= s->B) { ee_set_error("bad sequence index"); return EE_ERR_ARG; }
+  SessionRules& R = s->rules;
+  if (!R.h_hist) { ee_set_error("rules are not attached (ee_rules_attach)"); return EE_ERR_STATE; }
+  const int vocab = s->m->cfg.vocab;
+  float p[4] = {1.f, 0.f, 0.f, 1.f};
+  std::vector<int> tok(R.max_bias, -1);
+  std::vector<float> val(R.max_bias, 0.f);
+  RuleSlot q;
+  if (r) {
+    const float most = 1e6f;                             // (also refuses NaN)
+    if (!(r->repetition >= 1 / most && r->repetition <= most) || !(r->temperature >= 1 / most && r->temperature <= most)) {
+      ee_set_error("repetition and temperature must be positive, between 1e-6 and 1e6"); return EE_ERR_ARG;
+    }
+    if (!(r->frequency >= -most && r->frequency <= most) || !(r->presence >= -most && r->presence <= most)) {
+      ee_set_error("frequency and presence must be finite, at most 1e6"); return EE_ERR_ARG;
+    }
+    if (r->n_bias < 0 || r->n_bias > R.max_bias || (r->n_bias > 0 && (!r->bias_token || !r->bias_value))) {
+      ee_set_error("%d biases: room for %d was attached", r->n_bias, R.max_bias); return EE_ERR_ARG;
+    }
+    for (int i = 0; i < r->n_bias; ++i) {
+      if (r->bias_token[i] < 0 || r->bias_token[i] >= vocab) { ee_set_error("biased token out of range"); return EE_ERR_ARG; }
+      if (!(r->bias_value[i] >= -most && r->bias_value[i] <= most)) { ee_set_error("biases must be finite, at most 1e6"); return EE_ERR_ARG; }
+      tok[i] = r->bias_token[i]; val[i] = r->bias_value[i];
+    }
+    if (r->allowed) {
+      q.allowed.assign(r->allowed, r->allowed + R.words);
+      if (!tidy_mask(q.allowed.data(), R.words, vocab)) { ee_set_error("the mask allows no token"); return EE_ERR_ARG; }
+    }
+    q.on = true;
+    p[0] = r->repetition; p[1] = r->frequency; p[2] = r->presence; p[3] = r->temperature;
+  }
+  for (int i = 0; i < 4; ++i) HIP_TRY(hipMemcpyAsync(R.param + (size_t)i * s->B + seq, p + i, sizeof(float), hipMemcpyHostToDevice, s->st));
+  if (R.max_bias) {
+    HIP_TRY(hipMemcpyAsync(R.bias_token + (size_t)seq * R.max_bias, tok.data(), tok.size() * sizeof(int), hipMemcpyHostToDevice, s->st));
+    HIP_TRY(hipMemcpyAsync(R.bias_value + (size_t)seq * R.max_bias, val.data(), val.size() * sizeof(float), hipMemcpyHostToDevice, s->st));
+  }
+  if (!q.allowed.empty())
+    HIP_TRY(hipMemcpyAsync(R.mask + (size_t)seq * (s->max_rows + 1) * R.words, q.allowed.data(), q.allowed.size() * 4, hipMemcpyHostToDevice, s->st));
+  HIP_TRY(hipStreamSynchronize(s->st));
+  R.n_on += (int)q.on - (int)R.slot[seq].on;
+  R.slot[seq] = q;
+  R.known[seq] = 0;
+  return EE_OK;
+}
+
+extern "C" int ee_rules_rows(ee_session* s, int seq, int n, const uint32_t* allowed) {
+  if (!s || seq < 0 || seq >= s->B) { ee_set_error("bad sequence index"); return EE_ERR_ARG; }
+  SessionRules& R = s->rules;
+  if (!R.h_hist) { ee_set_error("rules are not attached (ee_rules_attach)"); return EE_ERR_STATE; }
+  RuleSlot& q = R.slot[seq];
+  if (!q.on) { ee_set_error("sequence %d has no rules (ee_rules_set)", seq); return EE_ERR_STATE; }
+  if (n < 0 || n > s->max_rows || (n > 0 && !allowed)) { ee_set_error("%d masks do not fit max_rows %d", n, s->max_rows); return EE_ERR_ARG; }
+  std::vector<uint32_t> m(allowed, allowed + (size_t)n * R.words);
+  for (int j = 0; j < n; ++j) {
+    uint32_t* row = m.data() + (size_t)j * R.words;
+    for (size_t w = 0; w < q.allowed.size(); ++w) row[w] &= q.allowed[w];
+    if (!tidy_mask(row, R.words, s->m->cfg.vocab)) { ee_set_error("mask %d allows no token", j); return EE_ERR_ARG; }
+  }
+  if (n) {
+    HIP_TRY(hipMemcpyAsync(R.mask + ((size_t)seq * (s->max_rows + 1) + 1) * R.words, m.data(), m.size() * 4, hipMemcpyHostToDevice, s->st));
+    HIP_TRY(hipStreamSynchronize(s->st));
+  }
+  q.n_rows = n;
+  return EE_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
 // C ABI: rollback
 // ---------------------------------------------------------------------------------------------
 extern "C" int kv_rollback(ee_session* s, int seq, int group_mask, int new_len) {
@@ -1386,6 +1680,8 @@ extern "C" int kv_rollback(ee_session* s, int seq, int group_mask, int new_len) 
   q.n_pi = std::min(q.n_pi, (int)q.V.size());
   for (int g = 2; g < n; ++g) q.n_pu[g - 2] = std::min(q.n_pu[g - 2], q.cut[g] - q.cut[g + 1]);
   q.n_hd = 0; q.S.clear(); q.sampled = false;
+  q.n_prompt = std::min(q.n_prompt, nT);
+  forget_tokens(s, seq, nT);
   q.len[0] = q.len[1] = new_len;
   trim_pages(s, seq);
   return EE_OK;
