@@ -143,6 +143,21 @@ int ee_prefill(ee_session* s, const int32_t* tokens, const int32_t* lens, int32_
  * EE_ERR_CAPACITY if the pool cannot hold it; the session is unchanged then. */
 int ee_prefill_seq(ee_session* s, int seq, const int32_t* tokens, int len, int32_t* first_token);
 
+/* The same for every sequence with lens[b] > 0 (the others, lens[b] == 0, keep their state; tokens: host, those prompts packed in
+ * sequence order), where the cache may already hold the beginning of a prompt: src[b] >= 0 names the sequence whose
+ * context as it stands before the call begins like the new prompt (src[b] == b: its own, a conversation that goes on).  The
+ * whole pages of positions that both begin with alike, that every layer group of src[b] holds and that leave at least the prompt's
+ * last token to run, become pages of both (Sec. 3.2: only block tables change); the rest of the prompt is built.  src: host
+ * [batch], entries of -1 and the entries of sequences that keep their state share nothing.  first_token: host [batch], -1
+ * for a sequence that keeps its state.
+ * Shared pages are read by all and written by none: a sequence that was rolled back into one gets a copy of its own when it
+ * next appends there (a page of the pool; EE_ERR_CAPACITY as for any growth).
+ * ee_debug_write_kv writes a shared page for all of its sequences. */
+int ee_prefill_shared(ee_session* s, const int32_t* src, const int32_t* tokens, const int32_t* lens, int32_t* first_token);
+
+/* Leading pages of a sequence's block table that another sequence holds as well (-1: bad argument). */
+int ee_shared_pages(const ee_session* s, int seq);
+
 /* A finished request leaves its slot: the sequence's KV pages return to the shared pool (Sec. 3.2: only the
  * block table changes) and its tokens, lengths and pending blocks are dropped.  The slot is idle until
  * ee_prefill / ee_prefill_seq starts it again: the batch-wide calls (ee_draft*, ee_verify_*, ee_decode_ar)

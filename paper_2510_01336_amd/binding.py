@@ -17,7 +17,7 @@ import numpy as np
 __all__ = [
     "lib", "lib_path", "EEError", "ee_config", "ee_rules_call", "ee_rules", "make_config", "Model", "Session", "LogitRules",
     "ee_model_bytes", "ee_model_load", "ee_model_set_tensor", "ee_model_get_tensor_rows", "ee_model_free",
-    "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
+    "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_prefill_shared", "ee_shared_pages", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
     "ee_verify_intermediate", "ee_verify_intermediate_static", "ee_verify_full", "ee_verify_level", "ee_n_levels", "kv_rollback", "ee_sampling_bytes", "ee_sampling_attach",
     "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist",
     "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
@@ -33,7 +33,7 @@ TENSOR_IDS = {"emb": 0, "head": 1, "gfinal": 2, "g1": 3, "wq": 4, "wk": 5, "wv":
 
 EXPORTED_SYMBOLS = [
     "ee_model_bytes", "ee_model_load", "ee_model_set_tensor", "ee_model_get_tensor_rows", "ee_model_free",
-    "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
+    "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_prefill_shared", "ee_shared_pages", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
     "ee_verify_intermediate", "ee_verify_intermediate_static", "ee_verify_full", "ee_verify_level", "ee_n_levels", "kv_rollback", "ee_sampling_bytes", "ee_sampling_attach",
     "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist",
     "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
@@ -99,6 +99,8 @@ def _load():
         "ee_prefill": (C.c_int, [vp, i32p, i32p, i32p]),
         "ee_decode_ar": (C.c_int, [vp, C.c_int, i32p]),
         "ee_prefill_seq": (C.c_int, [vp, C.c_int, i32p, C.c_int, i32p]),
+        "ee_prefill_shared": (C.c_int, [vp, i32p, i32p, i32p, i32p]),
+        "ee_shared_pages": (C.c_int, [vp, C.c_int]),
         "ee_seq_release": (C.c_int, [vp, C.c_int]),
         "ee_free_pages": (C.c_int, [vp]),
         "ee_draft": (C.c_int, [vp, C.c_int, i32p]),
@@ -258,6 +260,20 @@ def ee_prefill(session: int, tokens: np.ndarray, lens: np.ndarray) -> np.ndarray
     first = np.empty(len(l), np.int32)
     _chk(lib.ee_prefill(session, _p_i32(t), _p_i32(l), _p_i32(first)))
     return first
+
+
+def ee_prefill_shared(session: int, src: np.ndarray, tokens: np.ndarray, lens: np.ndarray) -> np.ndarray:
+    r, t, l = _i32(src), _i32(tokens), _i32(lens)
+    first = np.empty(len(l), np.int32)
+    _chk(lib.ee_prefill_shared(session, _p_i32(r), _p_i32(t), _p_i32(l), _p_i32(first)))
+    return first
+
+
+def ee_shared_pages(session: int, seq: int) -> int:
+    n = int(lib.ee_shared_pages(session, seq))
+    if n < 0:
+        raise EEError(-1, ee_last_error())
+    return n
 
 
 def ee_seq_release(session: int, seq: int) -> None:
@@ -652,6 +668,20 @@ class Session:
 
     def prefill_seq(self, seq: int, prompt: np.ndarray) -> int:
         return ee_prefill_seq(self.handle, seq, prompt)
+
+    def prefill_shared(self, src: Sequence[int], prompts: Sequence[Optional[np.ndarray]]) -> np.ndarray:
+        """Start (or restart) the sequences that have a prompt (None: keep); sequence b shares what the cache of sequence src[b] already
+        holds of it in whole pages (-1: nothing)."""
+        if len(src) != self.batch or len(prompts) != self.batch:
+            raise ValueError(f"a source and a prompt (or None) for each of {self.batch} sequences")
+        empty = np.zeros(0, np.int32)
+        given = [empty if p is None else _i32(p).reshape(-1) for p in prompts]
+        if any(p is not None and len(g) == 0 for p, g in zip(prompts, given)):
+            raise ValueError("a prompt is empty")
+        return ee_prefill_shared(self.handle, src, np.concatenate(given), np.array([len(g) for g in given], np.int32))
+
+    def shared_pages(self, seq: int) -> int:
+        return ee_shared_pages(self.handle, seq)
 
     def release(self, seq: int) -> None:
         ee_seq_release(self.handle, seq)

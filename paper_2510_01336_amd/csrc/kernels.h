@@ -24,6 +24,9 @@ void k_read_kv(hipStream_t st, bool bf16, const void* kv, const int* pages, int 
 void k_write_kv(hipStream_t st, bool bf16, void* kv, const int* pages, int layer, int pos0, int n, int n_pages, int n_kv, int D,
                 const float* k_in, const float* v_in);
 
+// page `to` of every layer <- page `from`; bytes: of one layer's page (a multiple of 16)
+void k_copy_page(hipStream_t st, void* kv, size_t bytes, int n_layers, int n_pages, int from, int to);
+
 // ---- fp32 reference-precision path (EE_F32 models) -----------------------------------------
 // rows of a pass into X (embedding of tok, rows[row_idx], or as they stand), cs[r][i] = (cos, sin)(pos_r * inv_freq[i]), rowinfo[r] =
 // (first q-tile of the row's sequence, row inside the sequence, KV page, slot in page)

@@ -86,6 +86,21 @@ void k_fill_nan_dead_kv(hipStream_t st, bool bf16, void* kv, const int* pages, i
                      layer0, layer1, n_pages, n_kv, D);
 }
 
+// One workgroup per 16 KiB of a layer's page: 32 layers of the 8B shape are 8.4 MB read and written.
+__global__ __launch_bounds__(256) void copy_page_kernel(uint4* kv, size_t units, int n_pages, int from, int to) {
+  const uint4* src = kv + ((size_t)blockIdx.y * n_pages + from) * units;
+  uint4* dst = kv + ((size_t)blockIdx.y * n_pages + to) * units;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const size_t i = (size_t)blockIdx.x * 1024 + j * 256 + threadIdx.x;
+    if (i < units) dst[i] = src[i];
+  }
+}
+void k_copy_page(hipStream_t st, void* kv, size_t bytes, int n_layers, int n_pages, int from, int to) {
+  const size_t units = bytes / 16;
+  hipLaunchKernelGGL(copy_page_kernel, dim3((unsigned)((units + 1023) / 1024), n_layers), dim3(256), 0, st, (uint4*)kv, units, n_pages, from, to);
+}
+
 __global__ void read_kv_kernel(const void* kv, int bf16, const int* pages, int layer, int pos0, int n, int n_pages, int n_kv,
                                int D, float* k_out, float* v_out) {
   int i = blockIdx.x * blockDim.x + threadIdx.x;

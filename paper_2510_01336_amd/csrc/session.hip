@@ -97,6 +97,7 @@ struct ee_session {
   int* out_host = nullptr;    // pinned, written by the kernels that decide them: n_accept[B], next[B], draft [B*max_rows]
   std::vector<SeqState> seq;
   std::vector<int> free_pages;
+  std::vector<int> page_ref;          // sequences that hold a page (more than one: shared, read only)
   bool debug_logits = false, time_kernels = false;
   int last_rows = 0, last_row0 = 0;   // rows of X behind the last exit head
   int last_attn = -1;                 // attention kernel of the last pass (ATTN_*; fp32: -1)
@@ -259,6 +260,7 @@ extern "C" int ee_session_create(ee_model* m, int batch, int max_ctx, int max_ro
   s->seq.resize(batch);
   s->free_pages.resize(s->n_pages);
   for (int i = 0; i < s->n_pages; ++i) s->free_pages[i] = s->n_pages - 1 - i;   // pop_back hands out 0, 1, 2, ...
+  s->page_ref.assign(s->n_pages, 0);
   *out = s;
   return EE_OK;
 }
@@ -281,11 +283,25 @@ extern "C" void ee_session_free(ee_session* s) {
 // ---------------------------------------------------------------------------------------------
 // pages
 // ---------------------------------------------------------------------------------------------
+static int take_page(ee_session* s) {
+  const int pg = s->free_pages.back();
+  s->free_pages.pop_back();
+  s->page_ref[pg] = 1;
+  return pg;
+}
+static void drop_page(ee_session* s, int pg) {
+  if (--s->page_ref[pg] == 0) s->free_pages.push_back(pg);
+}
+// pages that a call has to take for its sequences to hold positions [0, want_positions[b]) (0: not taking part), pages of their own
+// from the pending token's position on
 static int pages_needed_total(const ee_session* s, const std::vector<int>& want_positions) {
   int need = 0;
   for (int b = 0; b < s->B; ++b) {
-    int have = (int)s->seq[b].pages.size(), want = ceil_div(want_positions[b], EE_PAGE);
+    const SeqState& q = s->seq[b];
+    int have = (int)q.pages.size(), want = ceil_div(want_positions[b], EE_PAGE);
     if (want > have) need += want - have;
+    if (want_positions[b] > 0)
+      for (int i = std::max(0, (int)(q.C.size() + q.V.size()) - 1) / EE_PAGE; i < have; ++i) need += s->page_ref[q.pages[i]] > 1;
   }
   return need;
 }
@@ -294,8 +310,22 @@ static int grow_pages(ee_session* s, int b, int n) {
   SeqState& q = s->seq[b];
   while ((int)q.pages.size() * EE_PAGE < n) {
     if (s->free_pages.empty() || (int)q.pages.size() >= s->pps) { ee_set_error("KV page pool exhausted"); return EE_ERR_CAPACITY; }
-    q.pages.push_back(s->free_pages.back());
-    s->free_pages.pop_back();
+    q.pages.push_back(take_page(s));
+  }
+  return EE_OK;
+}
+// Before positions from p0 on are written: what sequence b holds there jointly with others (it was rolled back into a shared page) becomes
+// a page of its own with the same contents.
+static int own_pages(ee_session* s, int b, int p0) {
+  SeqState& q = s->seq[b];
+  for (size_t i = p0 / EE_PAGE; i < q.pages.size(); ++i) {
+    const int pg = q.pages[i];
+    if (s->page_ref[pg] < 2) continue;
+    if (s->free_pages.empty()) { ee_set_error("KV page pool exhausted"); return EE_ERR_CAPACITY; }
+    q.pages[i] = take_page(s);
+    drop_page(s, pg);
+    const ee_config& c = s->m->cfg;
+    k_copy_page(s->st, s->kv, (size_t)c.n_kv_heads * 2 * EE_PAGE * kv_page_dim(c.head_dim) * (s->m->bf16 ? 2 : 4), c.n_layers, s->n_pages, pg, q.pages[i]);
   }
   return EE_OK;
 }
@@ -312,7 +342,7 @@ static void settle(const ee_session* s, SeqState& q) {
 static void trim_pages(ee_session* s, int b) {
   SeqState& q = s->seq[b];
   int keep = ceil_div(max_len(s, q) + 1, EE_PAGE);
-  while ((int)q.pages.size() > keep) { s->free_pages.push_back(q.pages.back()); q.pages.pop_back(); }
+  while ((int)q.pages.size() > keep) { drop_page(s, q.pages.back()); q.pages.pop_back(); }
 }
 static int check_capacity(ee_session* s, const std::vector<int>& want_positions) {
   for (int b = 0; b < s->B; ++b)
@@ -359,6 +389,8 @@ static int build_meta(ee_session* s, int si, CallPlan& p, RowFn row_fn, int unif
     h[s->o_n_cand + b] = 0;
     if (m == 0) continue;
     p.max_m = std::max(p.max_m, m);
+    for (size_t i = p.p0[b] / EE_PAGE; i < s->seq[b].pages.size(); ++i)
+      if (s->page_ref[s->seq[b].pages[i]] > 1) { ee_set_error("internal: sequence %d would write a shared page", b); return EE_ERR_STATE; }
     for (int r = 0; r < m; ++r, ++row) {
       h[s->o_row_seq + row] = b; h[s->o_row_pos + row] = p.p0[b] + r;
       int tok = 0, src = 0, dst = 0;
@@ -767,7 +799,8 @@ static int finish(ee_session* s) {
 // ---------------------------------------------------------------------------------------------
 // (Re)start the sequences with lens[b] > 0 from their prompts (tokens: those prompts packed in sequence order);
 // sequences with lens[b] == 0 keep their state.  Pages of a restarted sequence go back to the pool first.
-static int prefill_impl(ee_session* s, const int32_t* tokens, const int32_t* lens, int32_t* first_token) {
+// src (or null): sequences whose cached beginnings they may share.
+static int prefill_impl(ee_session* s, const int32_t* tokens, const int32_t* lens, int32_t* first_token, const int32_t* src = nullptr) {
   const ee_config& c = s->m->cfg;
   std::vector<int> want(s->B);
   size_t total = 0;
@@ -778,22 +811,38 @@ static int prefill_impl(ee_session* s, const int32_t* tokens, const int32_t* len
   }
   for (size_t i = 0; i < total; ++i)
     if (tokens[i] < 0 || tokens[i] >= c.vocab) { ee_set_error("token id out of range"); return EE_ERR_ARG; }
+  // whole pages of positions that the source holds in every layer group and whose tokens the prompt begins with, the last token left to run
+  std::vector<std::vector<int>> joint(s->B);
+  for (size_t b = 0, off = 0; b < (size_t)s->B; off += std::max(0, lens[b]), ++b) {
+    if (lens[b] <= 0 || !src || src[b] < 0) continue;
+    const SeqState& q = s->seq[src[b]];
+    int n = std::min((int)q.C.size(), lens[b] - 1);
+    for (int g = 0; g <= s->n_levels; ++g) n = std::min(n, q.len[g]);
+    n = (int)(std::mismatch(q.C.begin(), q.C.begin() + std::max(0, n), tokens + off).first - q.C.begin());
+    joint[b].assign(q.pages.begin(), q.pages.begin() + n / EE_PAGE);
+  }
   // capacity is checked against the pool as it will be once the restarted sequences have given their pages back
   {
-    size_t freed = 0, need = 0;
+    std::vector<int> ref = s->page_ref;
+    size_t need = 0, avail = s->free_pages.size();
     for (int b = 0; b < s->B; ++b) {
       if (lens[b] <= 0) continue;
       if (want[b] > s->max_ctx) { ee_set_error("sequence %d would need %d positions (max_ctx %d)", b, want[b], s->max_ctx); return EE_ERR_CAPACITY; }
-      freed += s->seq[b].pages.size();
-      need += (size_t)ceil_div(want[b], EE_PAGE);
+      for (int pg : s->seq[b].pages) ref[pg]--;
+      for (int pg : joint[b]) ref[pg]++;
+      need += (size_t)ceil_div(want[b], EE_PAGE) - joint[b].size();
     }
-    if (need > s->free_pages.size() + freed) { ee_set_error("KV page pool exhausted"); return EE_ERR_CAPACITY; }
+    for (int pg = 0; pg < s->n_pages; ++pg) avail += s->page_ref[pg] > 0 && ref[pg] == 0;
+    if (need > avail) { ee_set_error("KV page pool exhausted"); return EE_ERR_CAPACITY; }
   }
+  for (int b = 0; b < s->B; ++b)
+    for (int pg : joint[b]) s->page_ref[pg]++;
   for (int b = 0; b < s->B; ++b) {
     if (lens[b] <= 0) continue;
     SeqState& q = s->seq[b];
-    for (int pg : q.pages) s->free_pages.push_back(pg);
+    for (int pg : q.pages) drop_page(s, pg);
     q = SeqState();
+    q.pages = joint[b];
     q.n_prompt = lens[b];
     forget_tokens(s, b, 0);
   }
@@ -806,6 +855,7 @@ static int prefill_impl(ee_session* s, const int32_t* tokens, const int32_t* len
       off0[b] = o;
       if (lens[b] <= 0) continue;
       o += lens[b];
+      done[b] = (int)joint[b].size() * EE_PAGE;
       EE_TRY(grow_pages(s, b, want[b]));
     }
   }
@@ -932,13 +982,38 @@ extern "C" int ee_prefill_seq(ee_session* s, int seq, const int32_t* tokens, int
   return EE_OK;
 }
 
+extern "C" int ee_prefill_shared(ee_session* s, const int32_t* src, const int32_t* tokens, const int32_t* lens, int32_t* first_token) {
+  if (!s || !src || !tokens || !lens || !first_token) { ee_set_error("null argument"); return EE_ERR_ARG; }
+  bool any = false;
+  for (int b = 0; b < s->B; ++b) {
+    if (lens[b] < 0) { ee_set_error("prompt %d has a negative length", b); return EE_ERR_ARG; }
+    if (lens[b] == 0) continue;
+    any = true;
+    if (src[b] < -1 || src[b] >= s->B) { ee_set_error("sequence %d: bad source %d", b, src[b]); return EE_ERR_ARG; }
+    if (src[b] >= 0 && !s->seq[src[b]].started) { ee_set_error("sequence %d: its source %d has no context", b, src[b]); return EE_ERR_STATE; }
+  }
+  if (!any) { ee_set_error("no prompt is given"); return EE_ERR_ARG; }
+  std::vector<int32_t> first(s->B, -1);
+  EE_TRY(prefill_impl(s, tokens, lens, first.data(), src));
+  std::copy(first.begin(), first.end(), first_token);
+  return EE_OK;
+}
+
+extern "C" int ee_shared_pages(const ee_session* s, int seq) {
+  if (!s || seq < 0 || seq >= s->B) { ee_set_error("bad sequence index"); return -1; }
+  const std::vector<int>& pages = s->seq[seq].pages;
+  size_t n = 0;
+  while (n < pages.size() && s->page_ref[pages[n]] > 1) ++n;
+  return (int)n;
+}
+
 // ---------------------------------------------------------------------------------------------
 // C ABI: vanilla greedy generation at full depth (Sec. 3.1)
 // ---------------------------------------------------------------------------------------------
 extern "C" int ee_seq_release(ee_session* s, int seq) {
   if (!s || seq < 0 || seq >= s->B) { ee_set_error("bad sequence index"); return EE_ERR_ARG; }
   SeqState& q = s->seq[seq];
-  while (!q.pages.empty()) { s->free_pages.push_back(q.pages.back()); q.pages.pop_back(); }
+  while (!q.pages.empty()) { drop_page(s, q.pages.back()); q.pages.pop_back(); }
   q = SeqState();
   forget_tokens(s, seq, 0);
   return EE_OK;
@@ -968,6 +1043,7 @@ extern "C" int ee_decode_ar(ee_session* s, int n, int32_t* out) {
     if (!s->seq[b].started) continue;
     p.m[b] = 1;
     p.p0[b] = (int)s->seq[b].C.size() - 1;          // the pending token's position
+    EE_TRY(own_pages(s, b, p.p0[b]));
     EE_TRY(grow_pages(s, b, want[b]));
   }
   EE_TRY(build_meta(s, 0, p, [&](int b, int, int& tok, int&, int&) { tok = s->seq[b].C.back(); }));
@@ -1049,6 +1125,7 @@ static int draft_impl(ee_session* s, int k, int32_t* draft, const float* u) {
     if (!q.started) continue;
     p.m[b] = 1;
     p.p0[b] = (int)(q.C.size() + q.V.size()) - 1;
+    EE_TRY(own_pages(s, b, p.p0[b]));
     EE_TRY(grow_pages(s, b, p.p0[b] + rows + 1));
   }
   EE_TRY(build_meta(s, 0, p, [&](int b, int, int& tok, int&, int& dst) {
@@ -1114,6 +1191,7 @@ extern "C" int ee_draft_inject(ee_session* s, int k, const int32_t* draft) {
     if (!q.started) continue;                         // an idle slot's entries of `draft` are ignored
     p.m[b] = rows;
     p.p0[b] = (int)(q.C.size() + q.V.size()) - 1;
+    EE_TRY(own_pages(s, b, p.p0[b]));
     EE_TRY(grow_pages(s, b, p.p0[b] + rows + 1));
   }
   EE_TRY(build_meta(s, 0, p, [&](int b, int r, int& tok, int&, int& dst) {
@@ -1799,10 +1877,13 @@ extern "C" int ee_debug_poison_dead_kv(ee_session* s, int seq) {
   const ee_config& c = s->m->cfg;
   const SeqState& q = s->seq[seq];
   EE_TRY(upload_pages(s, seq));
+  // (pages behind the last one of its own are shared and stay: what is dead here may be live elsewhere)
+  int own = (int)q.pages.size();
+  while (own > 0 && s->page_ref[q.pages[own - 1]] > 1) --own;
   std::vector<int> bounds = {0};
   bounds.insert(bounds.end(), s->m->exits.begin(), s->m->exits.end());
   for (int g = 0; g <= s->n_levels; ++g)
-    k_fill_nan_dead_kv(s->st, s->m->bf16, s->kv, s->page_scratch, (int)q.pages.size(), q.len[g], bounds[g], bounds[g + 1],
+    k_fill_nan_dead_kv(s->st, s->m->bf16, s->kv, s->page_scratch, own, q.len[g], bounds[g], bounds[g + 1],
                        s->n_pages, c.n_kv_heads, c.head_dim);
   HIP_TRY(hipGetLastError());
   HIP_TRY(hipStreamSynchronize(s->st));
