@@ -152,7 +152,8 @@ int ee_prefill_seq(ee_session* s, int seq, const int32_t* tokens, int len, int32
  * for a sequence that keeps its state.
  * Shared pages are read by all and written by none: a sequence that was rolled back into one gets a copy of its own when it
  * next appends there (a page of the pool; EE_ERR_CAPACITY as for any growth).
- * ee_debug_write_kv writes a shared page for all of its sequences. */
+ * ee_debug_write_kv writes a shared page for all of its sequences.  Draft, verification and decoding calls of bf16 models read pages
+ * that several of their sequences share once for all of them where that is quicker (results agree to rounding order). */
 int ee_prefill_shared(ee_session* s, const int32_t* src, const int32_t* tokens, const int32_t* lens, int32_t* first_token);
 
 /* Leading pages of a sequence's block table that another sequence holds as well (-1: bad argument). */
@@ -281,6 +282,22 @@ int ee_verify_level_rs(ee_session* s, int level, const uint8_t* active, const fl
  * verify call ee_debug_last_logits returns that call's target distributions instead of logits. */
 int ee_debug_read_dist(ee_session* s, int which, int seq, int row0, int n, float* host_out);
 
+/* ---- attention of given query rows over the cache ---------------------------------------------
+ * For readers of the cache outside the model (a draft head of its own, a probe): rows[b] query rows of sequence b at
+ * positions pos0[b] .. pos0[b]+rows[b]-1, row i attending to the cached positions 0 .. pos0[b]+i of one layer; query heads share the
+ * KV heads as in the model, scale 1/sqrt(head_dim).  The pages that several of the sequences share are read once for all their rows.
+ * ee_attend_begin fixes the rows for the ee_attend calls that follow (one per layer, say) and uploads what they need; pos0 null: the
+ * last rows[b] positions of group G1.  rows, pos0: host [batch]; rows[b] == 0 takes no part, rows[b] <= max_rows.  Any call that
+ * moves the session on (draft, verification, rollback, prompts, release) ends the validity of ee_attend_begin.
+ * q, out: device, the rows packed sequence by sequence, element (row, head, dim) at row*stride + head*head_dim + dim, of the
+ * model's dtype (EE_F32 or EE_BF16); strides in elements.  EE_BF16: q and out 16-byte aligned, strides multiples of 8.  out may not
+ * overlap q.  Nothing is synchronised: the calls can be captured into a graph and replayed while ee_attend_begin
+ * stays valid (work buffers are the session's: graphs and calls of one session may not overlap in time).
+ * EE_ERR_ARG: bad rows, positions or layer, or the layer's group does not hold the positions; EE_ERR_STATE: no valid begin,
+ * or a sequence without a context. */
+int ee_attend_begin(ee_session* s, const int32_t* rows, const int32_t* pos0);
+int ee_attend(ee_session* s, int layer, const void* q, int dtype, int64_t q_stride, void* out, int64_t out_stride);
+
 /* ---- decoding rules ------------------------------------------------------------------------------
  * What a caller asks of the next token besides the model's own preference, applied to a row's logits in this order, every step
  * rounded to fp32 (c: how often the token stands in the history behind the prompt):
@@ -406,9 +423,12 @@ int ee_debug_attention_split_pages(int pages);
 
 /* Test support, process-wide: the attention kernel of every bf16 call -- 0 KV splits with a merge, 1 blocks of 128 query rows,
  * 2 a wave per page (1 and 2 unsplit; all three serve any call) -- or -1, the built-in choice.  EE_ERR_ARG for any other
- * value.  ee_debug_last_attention returns the one that the session's last pass took (-1 before the first and for fp32). */
+ * value.  ee_debug_last_attention returns the one that the session's last pass took (-1 before the first and for fp32; 3: shared
+ * pages once for all their sequences).  ee_debug_shared_attention, process-wide: 1 takes that form wherever sequences of a call share
+ * pages, 0 never, -1 restores the built-in choice; a forced form or split length of the two calls above goes first. */
 int ee_debug_attention_form(int form);
 int ee_debug_last_attention(const ee_session* s);
+int ee_debug_shared_attention(int mode);
 
 /* Plain device-to-device streaming copy on `stream` (pointers and size multiples of 16 bytes; not
  * synchronised).  A kernel of exactly known traffic -- `bytes` read, `bytes` written -- used to

@@ -19,10 +19,10 @@ __all__ = [
     "ee_model_bytes", "ee_model_load", "ee_model_set_tensor", "ee_model_get_tensor_rows", "ee_model_free",
     "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_prefill_shared", "ee_shared_pages", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
     "ee_verify_intermediate", "ee_verify_intermediate_static", "ee_verify_full", "ee_verify_level", "ee_n_levels", "kv_rollback", "ee_sampling_bytes", "ee_sampling_attach",
-    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist",
+    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist", "ee_attend_begin", "ee_attend",
     "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
     "ee_debug_enable_logits", "ee_debug_last_logits", "ee_debug_last_hidden", "ee_debug_read_kv", "ee_debug_write_kv",
-    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
+    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_shared_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
     "EE_F32", "EE_BF16", "TENSOR_IDS", "EXPORTED_SYMBOLS",
 ]
 
@@ -35,10 +35,10 @@ EXPORTED_SYMBOLS = [
     "ee_model_bytes", "ee_model_load", "ee_model_set_tensor", "ee_model_get_tensor_rows", "ee_model_free",
     "ee_session_bytes", "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_seq", "ee_prefill_shared", "ee_shared_pages", "ee_seq_release", "ee_free_pages", "ee_decode_ar", "ee_draft", "ee_draft_inject",
     "ee_verify_intermediate", "ee_verify_intermediate_static", "ee_verify_full", "ee_verify_level", "ee_n_levels", "kv_rollback", "ee_sampling_bytes", "ee_sampling_attach",
-    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist",
+    "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist", "ee_attend_begin", "ee_attend",
     "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
     "ee_debug_enable_logits", "ee_debug_last_logits", "ee_debug_last_hidden", "ee_debug_read_kv", "ee_debug_write_kv",
-    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
+    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_shared_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
 ]
 
 
@@ -118,6 +118,9 @@ def _load():
         "ee_verify_intermediate_rs": (C.c_int, [vp, f32p, C.c_int, f32p, i32p, i32p]),
         "ee_verify_full_rs": (C.c_int, [vp, C.POINTER(C.c_uint8), f32p, C.c_int, f32p, i32p, i32p, i32p, i32p]),
         "ee_verify_level_rs": (C.c_int, [vp, C.c_int, C.POINTER(C.c_uint8), f32p, C.c_int, f32p, i32p, i32p, i32p, i32p]),
+        "ee_attend_begin": (C.c_int, [vp, i32p, i32p]),
+        "ee_attend": (C.c_int, [vp, C.c_int, vp, C.c_int, C.c_int64, vp, C.c_int64]),
+        "ee_debug_shared_attention": (C.c_int, [C.c_int]),
         "ee_logit_rules_bytes": (C.c_size_t, [C.c_int, C.c_int]),
         "ee_logit_rules": (C.c_int, [C.POINTER(ee_rules_call), vp]),
         "ee_rules_bytes": (C.c_size_t, [vp, C.c_int]),
@@ -407,6 +410,16 @@ def ee_verify_level_rs(session: int, level: int, batch: int, max_rows: int, u_ac
     return a, n, [com[b, :nc[b]].tolist() for b in range(batch)]
 
 
+def ee_attend_begin(session: int, rows: np.ndarray, pos0: Optional[np.ndarray] = None) -> None:
+    r = _i32(rows)
+    p = _i32(pos0) if pos0 is not None else None
+    _chk(lib.ee_attend_begin(session, _p_i32(r), _p_i32(p) if p is not None else None))
+
+
+def ee_attend(session: int, layer: int, q_ptr: int, dtype: int, q_stride: int, out_ptr: int, out_stride: int) -> None:
+    _chk(lib.ee_attend(session, layer, q_ptr, dtype, q_stride, out_ptr, out_stride))
+
+
 def ee_logit_rules_bytes(rows: int, vocab: int) -> int:
     return int(lib.ee_logit_rules_bytes(rows, vocab))
 
@@ -508,6 +521,10 @@ def ee_debug_attention_form(form: int) -> None:
 
 def ee_debug_last_attention(session: int) -> int:
     return lib.ee_debug_last_attention(session)
+
+
+def ee_debug_shared_attention(mode: int) -> None:
+    _chk(lib.ee_debug_shared_attention(int(mode)))
 
 
 def ee_debug_time_kernels(session: int, on: bool) -> None:
@@ -682,6 +699,41 @@ class Session:
 
     def shared_pages(self, seq: int) -> int:
         return ee_shared_pages(self.handle, seq)
+
+    def attend_begin(self, rows: Sequence[int], pos0: Optional[Sequence[int]] = None) -> None:
+        """Fix the query rows of the attend calls that follow: rows[b] of sequence b, at positions pos0[b] .. (default: its last ones)."""
+        if len(rows) != self.batch or (pos0 is not None and len(pos0) != self.batch):
+            raise ValueError(f"an entry for each of {self.batch} sequences")
+        ee_attend_begin(self.handle, rows, pos0)
+        self._attend_rows = int(sum(rows))
+
+    def attend(self, layer: int, q, out=None):
+        """Attention of the rows q [rows, query heads, head_dim] (the model's dtype) over one layer of the cache; out: of the same shape.
+        Ordered with torch's current stream of the device."""
+        import torch
+        cfg = self.model.cfg
+        dt = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
+        shape = (getattr(self, "_attend_rows", 0), cfg.n_q_heads, cfg.head_dim)
+        if out is None:
+            out = torch.empty(shape, dtype=dt, device=self._buf.device)
+        for name, t in (("q", q), ("out", out)):
+            if not torch.is_tensor(t) or t.dtype != dt or tuple(t.shape) != shape or t.device != self._buf.device:
+                raise ValueError(f"{name}: a {dt} tensor {list(shape)} on {self._buf.device}")
+            if t.stride(2) != 1 or (t.stride(1) != cfg.head_dim and cfg.n_q_heads > 1):
+                raise ValueError(f"{name}: the heads of a row side by side")
+        width = cfg.n_q_heads * cfg.head_dim
+        qs, os_ = (t.stride(0) if shape[0] > 1 else width for t in (q, out))
+        cur = torch.cuda.current_stream(q.device)
+        args = (self.handle, layer, q.data_ptr(), EE_BF16 if dt == torch.bfloat16 else EE_F32, qs, out.data_ptr(), os_)
+        if cur.cuda_stream == self.model.stream and torch.cuda.current_device() == q.device.index:
+            ee_attend(*args)
+            return out
+        with torch.cuda.device(q.device):
+            mine = torch.cuda.ExternalStream(self.model.stream) if self.model.stream else torch.cuda.default_stream(q.device)
+            mine.wait_stream(cur)
+            ee_attend(*args)
+            cur.wait_stream(mine)
+        return out
 
     def release(self, seq: int) -> None:
         ee_seq_release(self.handle, seq)

@@ -47,8 +47,9 @@ void f32_gemm(hipStream_t st, const float* X, int ldx, const float* g, float eps
 void f32_gate_up(hipStream_t st, const float* X, const float* g, float eps, const float* W, float* H, int M, int F, int d);
 // fused QKV: rotated Q rows, rotated K and V into their cache pages
 void f32_qkv(hipStream_t st, const float* X, const float* g, float eps, const float* W, int M, int d, const F32Out& out);
-void f32_attention(hipStream_t st, const float* Q, const float* kv, const CallMeta& meta, int pos_add, int M, int Hq, int Hkv,
-                   int D, int layer, int n_pages, int pages_per_seq, int max_ctx, float* out);
+// q and out: rows of the given strides (floats)
+void f32_attention(hipStream_t st, const float* Q, size_t q_stride, const float* kv, const CallMeta& meta, int pos_add, int M, int Hq, int Hkv,
+                   int D, int layer, int n_pages, int pages_per_seq, int max_ctx, float* out, size_t out_stride);
 void f32_argmax(hipStream_t st, const float* logits, int M, int V, int* v, const TakeToken& take);
 
 // ---- bf16 MFMA path (EE_BF16 models) ---------------------------------------------------------
@@ -121,7 +122,7 @@ void bf16_begin_pass(hipStream_t st, const bf16_t* emb, const int* tok, const fl
 struct AttnScratch { float* part_o; float* part_ml; int max_splits; };
 // Attention kernel and KV splits of a call (the same for all its layers), chosen from the sequence ends (kv_end[b] = first
 // position past the block, 0 for a sequence not taking part): every split takes `per` pages, the longest sequence has nsplit.
-enum { ATTN_RING = 0, ATTN_BLOCK, ATTN_TILE };
+enum { ATTN_RING = 0, ATTN_BLOCK, ATTN_TILE, ATTN_SHARED };      // (the last: by a SharedPlan, never part of an AttnPlan)
 struct AttnPlan { int kind, per, nsplit; };
 AttnPlan bf16_attention_plan(const int* kv_end, const int* seq_m, int B, int Hq, int Hkv, int max_splits);
 void bf16_attention(hipStream_t st, const AttnPlan& plan, const bf16_t* Q, const bf16_t* kv, const CallMeta& meta, int pos_add, int B,
@@ -147,3 +148,19 @@ size_t k_rules_workspace(int rows, int vocab);
 void k_rules(hipStream_t st, const ee_rules_call& call, const RulesStep& step);
 // dev[0..n) <- host (page-locked); token lists: list b of dst (stride entries) gets entries [delta[2b], delta[2b] + delta[2b+1]) of list b of src
 void k_rules_upload(hipStream_t st, const int* host, int* dev, int n, const int* src, int* dst, const int* delta, size_t stride, int B);
+
+// ---- attention over shared pages (kernels_shared.hip) ----
+// The tables are those of a SharedPlan (shared_plan.h) on the device.  by_rows: q and out row-major (out: strides in elements), else the
+// session's q-tiles and O-projection operand.
+struct SharedCall {
+  const bf16_t* kv = nullptr; const bf16_t* q = nullptr; bf16_t* out = nullptr;
+  bool by_rows = false;
+  int64_t q_stride = 0, out_stride = 0; int total_qt = 0, out_ktiles = 0;
+  const int* items = nullptr; const int4* rows = nullptr; const int4* joins = nullptr; const int* entries = nullptr;
+  int n_items = 0, n_joins = 0;
+  const int *seq_m = nullptr, *seq_p0 = nullptr, *block_table = nullptr;
+  int pos_add = 0, rep = 1, Hkv = 1, layer = 0, n_pages = 0, pps = 0;
+  float *part_o = nullptr, *part_ml = nullptr;         // [slot][KV head][16][D], [slot][KV head][16][2]
+};
+void k_shared_attention(hipStream_t st, const SharedCall& call, int D);
+void k_upload(hipStream_t st, const int* host, int* dev, int n);

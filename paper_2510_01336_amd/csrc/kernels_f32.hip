@@ -391,9 +391,9 @@ void f32_qkv(hipStream_t st, const float* X, const float* g, float eps, const fl
 // the threads of a dimension share out the positions in runs of eight; at a few dozen positions both products are one short
 // chain (the one-thread-per-position form took 10 us at 37 positions).  A head whose size is no multiple of 32 is padded as in
 // the pages, with zeros on both sides.
-__global__ __launch_bounds__(256) void f32_attention_kernel(const float* __restrict__ Q, const float* __restrict__ kv, const int* row_seq, const int* row_pos,
+__global__ __launch_bounds__(256) void f32_attention_kernel(const float* __restrict__ Q, size_t q_stride, const float* __restrict__ kv, const int* row_seq, const int* row_pos,
                                      const int* block_table, int pos_add, int Hq, int Hkv, int D, int layer, int n_pages,
-                                     int pps, float* __restrict__ out) {
+                                     int pps, float* __restrict__ out, size_t out_stride) {
   extern __shared__ float sm[];
   const int Dp = kv_page_dim(D);
   float* q = sm;                       // [Dp]
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(256) void f32_attention_kernel(const float* __restr
   const int r = blockIdx.x, h = blockIdx.y, kvh = h / (Hq / Hkv);
   const int n = row_pos[r] + pos_add + 1;
   const int* bt = block_table + row_seq[r] * pps;
-  for (int d = threadIdx.x; d < Dp; d += blockDim.x) q[d] = d < D ? Q[(size_t)r * Hq * D + h * D + d] : 0.f;
+  for (int d = threadIdx.x; d < Dp; d += blockDim.x) q[d] = d < D ? Q[r * q_stride + h * D + d] : 0.f;
   __syncthreads();
   const float scale = 1.0f / sqrtf((float)D);
   float mx = -INFINITY;
@@ -450,16 +450,16 @@ __global__ __launch_bounds__(256) void f32_attention_kernel(const float* __restr
     __syncthreads();
     if (ph == 0 && d < D) {
       for (int i = 1; i < phases; ++i) acc += part[i * min(D, 256) + threadIdx.x];
-      out[(size_t)r * Hq * D + h * D + d] = acc / sum;
+      out[r * out_stride + h * D + d] = acc / sum;
     }
     __syncthreads();
   }
 }
-void f32_attention(hipStream_t st, const float* Q, const float* kv, const CallMeta& meta, int pos_add, int M, int Hq, int Hkv,
-                   int D, int layer, int n_pages, int pages_per_seq, int max_ctx, float* out) {
+void f32_attention(hipStream_t st, const float* Q, size_t q_stride, const float* kv, const CallMeta& meta, int pos_add, int M, int Hq, int Hkv,
+                   int D, int layer, int n_pages, int pages_per_seq, int max_ctx, float* out, size_t out_stride) {
   const size_t smem = (size_t)(kv_page_dim(D) + 8 + 256 + max_ctx) * sizeof(float);
-  hipLaunchKernelGGL(f32_attention_kernel, dim3(M, Hq), dim3(256), smem, st, Q, kv, meta.row_seq, meta.row_pos, meta.block_table, pos_add,
-                     Hq, Hkv, D, layer, n_pages, pages_per_seq, out);
+  hipLaunchKernelGGL(f32_attention_kernel, dim3(M, Hq), dim3(256), smem, st, Q, q_stride, kv, meta.row_seq, meta.row_pos, meta.block_table, pos_add,
+                     Hq, Hkv, D, layer, n_pages, pages_per_seq, out, out_stride);
 }
 
 // arg max of each row; the lowest index wins ties.  Sixteen waves, eight values per thread in flight.

@@ -1,0 +1,313 @@
+// Attention of a batch whose sequences share pages: a page that the block tables of several sequences name is read once for the
+// query rows of all of them (see shared_plan.h for how a call is cut into items).
+//
+//   o = sum_j w_j V_j / sum_j w_j,  w_j = exp(q.K_j / sqrt(D));  over a run of pages: m = max of the scores (base 2), l = sum 2^(s_j - m),
+//   o' = sum 2^(s_j - m) V_j; runs join by m = max m_k, l = sum l_k 2^(m_k - m), o = sum o'_k 2^(m_k - m) / l.
+//
+// Operands are bf16, scores, statistics and accumulators fp32; the softmax weights are rounded to bf16 for the second matrix product (relative error
+// 2^-9 each, averaged over the positions) and the output once at the end.
+#include "kernels.h"
+#include <climits>
+#include <type_traits>
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+__device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t pack2(float lo, float hi) {
+  const f32x2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+// maximum over the four 16-lane rows of a wave, delivered to every lane
+__device__ inline float colmax4(float x) {
+  typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+  u32x2_t r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Query and output of a row: the session's own layouts (q-tiles in fragment order, the O projection's operand), or row-major
+// (element (row, head, dim) at row * stride + head * D + dim).
+template <int D, bool ROWS>
+__device__ inline const bf16_t* q_address(const SharedCall& a, int4 w, int kvh, int g) {
+  if (ROWS) return a.q + (size_t)max(w.x, 0) * a.q_stride + (size_t)(kvh * a.rep + w.y) * D + 8 * g;
+  return a.q + ((size_t)kvh * a.total_qt + (w.z >> 4)) * (D / 32 * 512) + (g * 16 + (w.z & 15)) * 8;
+}
+// four consecutive elements from dimension d of the output row
+template <int D, bool ROWS>
+__device__ inline void store_out(const SharedCall& a, int row, int head, int kvh, int d, float x, float y, float z, float w) {
+  const int col = (kvh * a.rep + head) * D + d;
+  bf16_t* p = ROWS ? a.out + (size_t)row * a.out_stride + col : a.out + act_offset(row, col, a.out_ktiles);
+  *(uint2*)p = make_uint2(pack2(x, y), pack2(z, w));
+}
+
+// Workgroup = (KV head, item): up to eight packed q-tiles and a run of pages.  Wave (qg, par) owns tiles 2*qg, 2*qg+1 and every second page; pages
+// reach LDS by direct global->LDS loads, two slots of two pages each, one barrier per pair of pages; the parities of a tile meet in LDS at the
+// end.
+template <int D, bool ROWS>
+__global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
+  constexpr int DS = D / 32, DT = D / 16, KCH = 4 * DS, CH = KCH + 2 * DT;     // 1 KiB chunks of a page: K first, then V
+  constexpr int CPW = CH / 4;                                                  // chunks a wave requests per step
+  __shared__ u32x4 lds[4][CH * 64];                                            // slot 2 * (step mod 2) + parity
+  __shared__ float2 ml[4][2][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, qc = lane & 15;
+  const int wave_s = __builtin_amdgcn_readfirstlane(wave), qg = wave_s & 3, par = wave_s >> 2;
+  const int kvh = blockIdx.x;
+  const int* it = a.items + 8 * blockIdx.y;
+  const int tile0 = it[0], n_tiles = it[1], seq = it[2], page0 = it[3], slot0 = it[5];
+  const bool own = it[6] != 0;
+  const int kv_end = own ? a.seq_p0[seq] + a.seq_m[seq] + a.pos_add : INT_MAX;
+  const int page1 = own ? min(it[4], (kv_end + EE_PAGE - 1) / EE_PAGE) : it[4];
+  if (page0 >= page1) {                                // a run that this step does not reach yet: nothing to join (whole workgroup)
+    if (slot0 >= 0 && threadIdx.x < n_tiles * 16)
+      *(float2*)(a.part_ml + (((size_t)(slot0 + (threadIdx.x >> 4)) * a.Hkv + kvh) * 16 + (threadIdx.x & 15)) * 2) = make_float2(-INFINITY, 0.f);
+    return;
+  }
+  const int npg = page1 - page0, nst = (npg + 1) >> 1;
+  const int* bt = a.block_table + (size_t)seq * a.pps + page0;
+  typedef const __attribute__((address_space(1))) void* gptr_t;
+  typedef __attribute__((address_space(3))) void* lptr_t;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lptr_t)&lds[0][0]);
+  auto request = [&](int step, int page) __attribute__((always_inline)) {
+    const u32x4* src = (const u32x4*)(a.kv + kv_slab(a.layer, page, kvh, a.n_pages, a.Hkv, D)) + qg * CPW * 64 + lane;
+    const unsigned dst = lds0 + 1024u * (((step & 1) * 2 + par) * CH + qg * CPW);
+#pragma unroll
+    for (int j = 0; j < CPW; ++j) __builtin_amdgcn_global_load_lds((gptr_t)(src + j * 64), (lptr_t)(size_t)(dst + 1024u * j), 16, 0, 0);
+  };
+  request(0, bt[min(par, npg - 1)]);
+  int next_page = bt[min(2 + par, npg - 1)];
+  // pages before this one are seen whole by every row of the item
+  const int first_masked = own ? (a.rows[tile0 * 16].w + a.pos_add + 1) / EE_PAGE - page0 : npg + 2;
+  bool has[2];
+  int limit[2];
+  int4 row[2];
+  u32x4 qf[2][DS];
+  float mrun[2];
+  f32x4 o[2][DT], lacc[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    has[i] = 2 * qg + i < n_tiles;
+    row[i] = a.rows[(tile0 + (has[i] ? 2 * qg + i : 0)) * 16 + qc];
+    limit[i] = row[i].x < 0 ? -1 : own ? row[i].w + a.pos_add : INT_MAX;
+    const bf16_t* q = q_address<D, ROWS>(a, row[i], kvh, g);
+#pragma unroll
+    for (int s = 0; s < DS; ++s) qf[i][s] = *(const u32x4*)(q + s * (ROWS ? 32 : 512));
+    mrun[i] = -INFINITY; lacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[i][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float sc2 = 1.4426950408889634f / sqrtf((float)D);         // scores in base-2 units
+  const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+  auto page_step = [&](auto masked_c, const u32x4* L, int pg) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked_c)::value;
+    const int base = (page0 + pg) * EE_PAGE + 16 * g;  // this lane group holds positions base .. base+15
+    f32x4 s4[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                      // (fragments in halves: 256 registers hold no more)
+      u32x4 kf[2 * DS];
+#pragma unroll
+      for (int c = 0; c < 2 * DS; ++c) kf[c] = L[(h * 2 * DS + c) * 64];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s4[i][2 * h + t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < DS; ++s)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) s4[i][2 * h + t] = mfma16(kf[t * DS + s], qf[i][s], s4[i][2 * h + t]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    u32x4 vf[DT];                                      // first half of V, requested under the softmax
+#pragma unroll
+    for (int c = 0; c < DT; ++c) vf[c] = L[(KCH + c) * 64];
+    u32x4 P[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          if (MASKED && base + 4 * t + v > limit[i]) s4[i][t][v] = -INFINITY;
+          tmax = fmaxf(tmax, s4[i][t][v]);
+        }
+      tmax = colmax4(tmax * sc2);
+      const float mnew = fmaxf(mrun[i], tmax);
+      const float msafe = mnew == -INFINITY ? 0.f : mnew;
+      const float alpha = __builtin_amdgcn_exp2f(mrun[i] - msafe), nm = -msafe;
+      mrun[i] = mnew;
+      uint32_t pk[8];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        pk[2 * t] = pack2(__builtin_amdgcn_exp2f(fmaf(s4[i][t][0], sc2, nm)), __builtin_amdgcn_exp2f(fmaf(s4[i][t][1], sc2, nm)));
+        pk[2 * t + 1] = pack2(__builtin_amdgcn_exp2f(fmaf(s4[i][t][2], sc2, nm)), __builtin_amdgcn_exp2f(fmaf(s4[i][t][3], sc2, nm)));
+      }
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {       // (rare once the maximum has settled)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) { o[i][dt][0] *= alpha; o[i][dt][1] *= alpha; o[i][dt][2] *= alpha; o[i][dt][3] *= alpha; }
+        lacc[i][0] *= alpha; lacc[i][1] *= alpha; lacc[i][2] *= alpha; lacc[i][3] *= alpha;
+      }
+      P[i][0] = u32x4{pk[0], pk[1], pk[2], pk[3]};
+      P[i][1] = u32x4{pk[4], pk[5], pk[6], pk[7]};
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (h) {
+#pragma unroll
+        for (int c = 0; c < DT; ++c) vf[c] = L[(KCH + DT + c) * 64];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) lacc[i] = mfma16(ones, P[i][h], lacc[i]);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int dt = 0; dt < DT / 2; ++dt) {
+          u32x4 v = vf[dt * 2 + ks];
+          if (MASKED) {     // dead positions (>= kv_end) may hold anything: zero their V
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int pa = base + 8 * ks + 2 * j;
+              v[j] &= pa + 1 < kv_end ? 0xffffffffu : (pa < kv_end ? 0xffffu : 0u);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) o[i][h * DT / 2 + dt] = mfma16(v, P[i][ks], o[i][h * DT / 2 + dt]);
+        }
+    }
+  };
+  auto open_step = [&](int st) __attribute__((always_inline)) {
+    // own requests of this step landed; behind the barrier everybody's, and everybody is done with the other two slots
+    __builtin_amdgcn_s_waitcnt(0x70);                  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (st + 1 < nst) {
+      request(st + 1, next_page);
+      next_page = bt[min(2 * (st + 2) + par, npg - 1)];
+    }
+    return &lds[0][0] + ((st & 1) * 2 + par) * (CH * 64) + lane;
+  };
+  int st = 0;
+  for (; 2 * st + 1 < first_masked && 2 * st + 1 < npg; ++st) {
+    const u32x4* L = open_step(st);
+    if (has[0]) page_step(std::false_type{}, L, 2 * st + par);
+  }
+  for (; st < nst; ++st) {
+    const u32x4* L = open_step(st);
+    if (has[0] && 2 * st + par < npg) page_step(std::true_type{}, L, 2 * st + par);
+  }
+  // the odd pages' partials through LDS to the waves of the even pages
+  __syncthreads();
+  f32x4* po = (f32x4*)&lds[0][0] + qg * (2 * DT * 64) + lane;
+  if (par == 1 && has[0]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ml[qg][i][lane] = make_float2(mrun[i], lacc[i][0]);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) po[(i * DT + dt) * 64] = o[i][dt];
+    }
+  }
+  __syncthreads();
+  if (par == 1) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (!has[i]) continue;
+    const float2 t = ml[qg][i][lane];
+    const float mm = fmaxf(mrun[i], t.x), ms = mm == -INFINITY ? 0.f : mm;
+    const float f0 = __builtin_amdgcn_exp2f(mrun[i] - ms), f1 = __builtin_amdgcn_exp2f(t.x - ms);
+    const float l = lacc[i][0] * f0 + t.y * f1;
+    if (slot0 < 0) {
+      if (row[i].x < 0) continue;
+      const float inv = 1.0f / l, a0 = f0 * inv, a1 = f1 * inv;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 x = po[(i * DT + dt) * 64];
+        store_out<D, ROWS>(a, row[i].x, row[i].y, kvh, dt * 16 + 4 * g, o[i][dt][0] * a0 + x[0] * a1, o[i][dt][1] * a0 + x[1] * a1,
+                           o[i][dt][2] * a0 + x[2] * a1, o[i][dt][3] * a0 + x[3] * a1);
+      }
+    } else {
+      const size_t at = ((size_t)(slot0 + 2 * qg + i) * a.Hkv + kvh) * 16 + qc;
+      if (g == 0) *(float2*)(a.part_ml + at * 2) = make_float2(mm, l);
+      float* p = a.part_o + at * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 x = po[(i * DT + dt) * 64];
+        *(f32x4*)(p + dt * 16) = f32x4{o[i][dt][0] * f0 + x[0] * f1, o[i][dt][1] * f0 + x[1] * f1, o[i][dt][2] * f0 + x[2] * f1, o[i][dt][3] * f0 + x[3] * f1};
+      }
+    }
+  }
+}
+
+// A wave per (row, KV head): the partials of the row's items, in the plan's order.
+template <int D, bool ROWS>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedCall a) {
+  constexpr int LPR = D / 4;                           // lanes of a row (four dimensions each); the wave's halves (quarters) share out the partials
+  const int lane = threadIdx.x & 63, w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = w % a.Hkv, j = w / a.Hkv;
+  if (j >= a.n_joins) return;                          // whole wave
+  const int4 jn = a.joins[j];                          // row, head, first entry, entries
+  const int sub = lane / LPR, d = (lane % LPR) * 4;
+  constexpr int SUBS = 64 / LPR;
+  float mx = -INFINITY;
+  for (int k = lane; k < jn.w; k += 64) {
+    const int e = a.entries[jn.z + k];
+    mx = fmaxf(mx, a.part_ml[(((size_t)(e >> 4) * a.Hkv + kvh) * 16 + (e & 15)) * 2]);
+  }
+  for (int s = 1; s < 64; s <<= 1) mx = fmaxf(mx, __shfl_xor(mx, s, 64));
+  float den = 0.f;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = sub; k < jn.w; k += SUBS) {
+    const int e = a.entries[jn.z + k];
+    const size_t at = ((size_t)(e >> 4) * a.Hkv + kvh) * 16 + (e & 15);
+    const float2 t = *(const float2*)(a.part_ml + at * 2);
+    const f32x4 x = *(const f32x4*)(a.part_o + at * D + d);
+    const float f = __builtin_amdgcn_exp2f(t.x - mx);
+    const bool some = t.y > 0.f;                       // (an item that this step did not reach has left no sum)
+    den += some ? f * t.y : 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) acc[v] += some ? f * x[v] : 0.f;
+  }
+#pragma unroll
+  for (int s = LPR; s < 64; s <<= 1) {
+    den += __shfl_xor(den, s, 64);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) acc[v] += __shfl_xor(acc[v], s, 64);
+  }
+  if (sub == 0) {
+    const float inv = 1.0f / den;
+    store_out<D, ROWS>(a, jn.x, jn.y, kvh, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  }
+}
+
+template <int D, bool ROWS>
+static void launch_shared(hipStream_t st, const SharedCall& a) {
+  hipLaunchKernelGGL((shared_attn_kernel<D, ROWS>), dim3(a.Hkv, a.n_items), dim3(512), 0, st, a);
+  if (a.n_joins > 0)
+    hipLaunchKernelGGL((shared_join_kernel<D, ROWS>), dim3((unsigned)(((size_t)a.n_joins * a.Hkv + 3) / 4)), dim3(256), 0, st, a);
+}
+void k_shared_attention(hipStream_t st, const SharedCall& a, int D) {
+  if (a.n_items <= 0) return;
+  if (D == 128) {
+    if (a.by_rows) launch_shared<128, true>(st, a); else launch_shared<128, false>(st, a);
+  } else {
+    if (a.by_rows) launch_shared<64, true>(st, a); else launch_shared<64, false>(st, a);
+  }
+}
+
+// dev[0..n) <- host (page-locked)
+__global__ __launch_bounds__(256) void upload_kernel(const int* __restrict__ host, int* __restrict__ dev, int n) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int i = blockIdx.x * 1024 + j * 256 + threadIdx.x;
+    if (i < n) dev[i] = host[i];
+  }
+}
+void k_upload(hipStream_t st, const int* host, int* dev, int n) {
+  if (n > 0) hipLaunchKernelGGL(upload_kernel, dim3(ceil_div(n, 1024)), dim3(256), 0, st, host, dev, n);
+}

@@ -2,6 +2,7 @@
 // with the KV-cache and hidden-state reuse of its Sec. 3.2).  Host code only decides shapes and
 // keeps the integer bookkeeping; every arithmetic step runs in the kernels of kernels_*.hip.
 #include "kernels.h"
+#include "shared_plan.h"
 #include <algorithm>
 #include <cstring>
 #include <mutex>
@@ -31,6 +32,23 @@ struct MetaSlot {             // one upload region: host (pinned) + device copy,
 };
 
 struct KTimer { int fam; hipEvent_t a, b; };
+
+struct SharedSlot;
+struct CallPlan {
+  int M = 0, max_m = 0, total_qt = 0;
+  std::vector<int> m, p0;        // per sequence rows and first position (m = 0: not taking part)
+  const SharedSlot* shared = nullptr;   // set: the attention reads shared pages once, by these tables
+};
+
+// Tables of a call whose attention reads shared pages once (SharedPlan): host (pinned) + device copy, one per metadata slot.
+struct SharedSlot {
+  int* h = nullptr;
+  int* d = nullptr;
+  hipEvent_t copied = nullptr;
+  bool in_flight = false;
+  int n_items = 0, n_joins = 0, slots = 0;
+  size_t o_rows = 0, o_joins = 0, o_entries = 0;
+};
 
 // Decoding rules of a session (ee_rules_*): the rules of every slot, and what lies in the attached arena.
 struct RuleSlot {
@@ -88,6 +106,11 @@ struct ee_session {
   // models, the operand of the up projection), that operand's unused sum-of-squares partials, unit gains
   float *Z = nullptr, *T = nullptr, *ssq_t = nullptr, *ones = nullptr;
   void* TF = nullptr;
+  SharedSlot shared[2];
+  size_t shared_cap = 0;        // ints of one of them
+  bool attend_ready = false;    // ee_attend_begin's metadata (slot 0) and tables are in place
+  std::vector<int> attend_end;  // positions that its rows see, per sequence (0: takes no part)
+  CallPlan attend;
   size_t part_units = 0;        // capacity of the attention split scratch in (q-tile, split) units per KV head
   int* pidx = nullptr;
   int max_splits = 64;
@@ -189,6 +212,11 @@ static size_t carve(ee_session* s, char* base) {
     s->gemm_part = s->maxM > 64 ? cv.take<float>(gp) : nullptr;
     s->inv_rms = cv.take<float>(s->inv_cap);
   }
+  if (bf) {      // rows of at most four segments each, items and entries of as many partials as there is room for
+    const size_t packed = 4 * (size_t)s->headM * rep + 16 * (size_t)s->B, joins = (size_t)s->headM * rep;
+    s->shared_cap = 4 * packed + 8 * (packed / 16 + s->part_units) + 4 * joins + 16 * s->part_units;
+    for (SharedSlot& sl : s->shared) sl.d = cv.take<int>(s->shared_cap);
+  }
   s->slot[0].d = cv.take<int>(s->meta_cap);
   s->slot[1].d = cv.take<int>(s->meta_cap - s->B * (s->max_rows + 1));     // (no uniform numbers there)
   (void)rep;
@@ -253,6 +281,8 @@ extern "C" int ee_session_create(ee_model* m, int batch, int max_ctx, int max_ro
   for (int i = 0; i < 2 && e == hipSuccess; ++i) {
     e = hipHostMalloc((void**)&s->slot[i].h, s->meta_cap * sizeof(int), hipHostMallocDefault);
     if (e == hipSuccess) e = hipEventCreateWithFlags(&s->slot[i].copied, hipEventDisableTiming);
+    if (e == hipSuccess && s->shared_cap) e = hipHostMalloc((void**)&s->shared[i].h, s->shared_cap * sizeof(int), hipHostMallocDefault);
+    if (e == hipSuccess && s->shared_cap) e = hipEventCreateWithFlags(&s->shared[i].copied, hipEventDisableTiming);
   }
   if (e == hipSuccess) e = hipHostMalloc((void**)&s->out_host, (2 * (size_t)batch + (size_t)batch * max_rows) * sizeof(int), hipHostMallocDefault);
   if (e == hipSuccess) e = hipStreamSynchronize(s->st);
@@ -272,6 +302,8 @@ extern "C" void ee_session_free(ee_session* s) {
   for (int i = 0; i < 2; ++i) {
     if (s->slot[i].h) (void)hipHostFree(s->slot[i].h);
     if (s->slot[i].copied) (void)hipEventDestroy(s->slot[i].copied);
+    if (s->shared[i].h) (void)hipHostFree(s->shared[i].h);
+    if (s->shared[i].copied) (void)hipEventDestroy(s->shared[i].copied);
   }
   if (s->out_host) (void)hipHostFree(s->out_host);
   if (s->rules.h_hist) (void)hipHostFree(s->rules.h_hist);
@@ -354,10 +386,6 @@ static int check_capacity(ee_session* s, const std::vector<int>& want_positions)
 // ---------------------------------------------------------------------------------------------
 // per-call metadata
 // ---------------------------------------------------------------------------------------------
-struct CallPlan {
-  int M = 0, max_m = 0, total_qt = 0;
-  std::vector<int> m, p0;        // per sequence rows and first position (m = 0: not taking part)
-};
 
 static CallMeta meta_ptrs(const ee_session* s, const int* d) {
   CallMeta c;
@@ -372,7 +400,8 @@ static CallMeta meta_ptrs(const ee_session* s, const int* d) {
 // Fill slot `si` from the plan: rows are packed sequence by sequence.  The callbacks give the
 // per-row token / gather source / scatter destination; candidates are filled by the caller.
 template <class RowFn>
-static int build_meta(ee_session* s, int si, CallPlan& p, RowFn row_fn, int uniforms = 0) {
+static int build_meta(ee_session* s, int si, CallPlan& p, RowFn row_fn, int uniforms = 0, bool writes = true) {
+  s->attend_ready = false;
   MetaSlot& sl = s->slot[si];
   if (sl.in_flight) { HIP_TRY(hipEventSynchronize(sl.copied)); sl.in_flight = false; }
   int* h = sl.h;
@@ -389,7 +418,7 @@ static int build_meta(ee_session* s, int si, CallPlan& p, RowFn row_fn, int unif
     h[s->o_n_cand + b] = 0;
     if (m == 0) continue;
     p.max_m = std::max(p.max_m, m);
-    for (size_t i = p.p0[b] / EE_PAGE; i < s->seq[b].pages.size(); ++i)
+    for (size_t i = p.p0[b] / EE_PAGE; writes && i < s->seq[b].pages.size(); ++i)
       if (s->page_ref[s->seq[b].pages[i]] > 1) { ee_set_error("internal: sequence %d would write a shared page", b); return EE_ERR_STATE; }
     for (int r = 0; r < m; ++r, ++row) {
       h[s->o_row_seq + row] = b; h[s->o_row_pos + row] = p.p0[b] + r;
@@ -414,6 +443,71 @@ static int upload_meta(ee_session* s, int si) {
   HIP_TRY(hipEventRecord(sl.copied, s->st));
   sl.in_flight = true;
   return EE_OK;
+}
+
+// Tables of the call in slot `si` for attention that reads shared pages once, where that is possible and quicker (always: also where
+// nothing is shared); steps: of a sequential pass.  Sets p.shared.  Called after build_meta.
+extern int g_shared_attention;
+int g_shared_attention = -1;         // test hook: 1 wherever pages are shared, 0 never, -1 the built-in choice
+static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool always = false) {
+  p.shared = nullptr;
+  if (!s->m->bf16) return EE_OK;
+  const int rep = s->m->cfg.n_q_heads / s->m->cfg.n_kv_heads;
+  if (!always) {
+    if (g_shared_attention == 0 || g_attn_form >= 0 || g_attn_pages_override > 0) return EE_OK;
+    bool any = false;
+    for (int b = 0; b < s->B && !any; ++b) any = p.m[b] > 0 && p.p0[b] >= EE_PAGE && s->page_ref[s->seq[b].pages[0]] > 1;
+    if (!any) return EE_OK;
+  }
+  std::vector<SharedSeq> q(s->B);
+  const int* h = s->slot[si].h;
+  for (int b = 0; b < s->B; ++b) {
+    if (!p.m[b]) continue;
+    q[b].m = p.m[b]; q[b].p0 = p.p0[b]; q[b].row0 = h[s->o_seq_row0 + b]; q[b].qt0 = h[s->o_seq_qt0 + b];
+    q[b].n_pages = ceil_div(p.p0[b] + p.m[b] + steps - 1, EE_PAGE);
+    q[b].pages = s->seq[b].pages.data();
+  }
+  const int wgs = std::max(1, 256 / s->m->cfg.n_kv_heads);
+  SharedPlan P = plan_shared(q, rep, (int)s->part_units, wgs, 2, true);
+  SharedSlot& sl = s->shared[si];
+  auto fits = [&](const SharedPlan& x) {
+    return 8 * x.items.size() + 4 * x.rows.size() + 4 * x.joins.size() + x.entries.size() + 16 <= s->shared_cap && (size_t)x.slots <= s->part_units;
+  };
+  if (!fits(P) && always) P = plan_shared(q, rep, (int)s->part_units, wgs, 2, false);      // (every sequence by itself, uncut if need be)
+  if (!fits(P)) {
+    if (always) { ee_set_error("internal: the tables of %d rows do not fit", p.M); return EE_ERR_CAPACITY; }
+    return EE_OK;
+  }
+  if (!always && (!P.shares || (g_shared_attention < 0 && !shared_pays(P)))) return EE_OK;
+  if (sl.in_flight) { HIP_TRY(hipEventSynchronize(sl.copied)); sl.in_flight = false; }
+  size_t o = 0;
+  auto put = [&](const void* src, size_t n) {
+    memcpy(sl.h + o, src, n * sizeof(int));
+    const size_t r = o;
+    o += (n + 3) / 4 * 4;
+    return r;
+  };
+  put(P.items.data(), 8 * P.items.size());
+  sl.o_rows = put(P.rows.data(), 4 * P.rows.size());
+  sl.o_joins = put(P.joins.data(), 4 * P.joins.size());
+  sl.o_entries = put(P.entries.data(), P.entries.size());
+  sl.n_items = (int)P.items.size(); sl.n_joins = (int)P.joins.size(); sl.slots = P.slots;
+  k_upload(s->st, sl.h, sl.d, (int)o);
+  HIP_TRY(hipEventRecord(sl.copied, s->st));
+  sl.in_flight = true;
+  p.shared = &sl;
+  return EE_OK;
+}
+static SharedCall shared_call(const ee_session* s, const SharedSlot& sl, const CallMeta& mt, int pos_add, int layer) {
+  const ee_config& c = s->m->cfg;
+  SharedCall a;
+  a.kv = (const bf16_t*)s->kv;
+  a.items = sl.d; a.rows = (const int4*)(sl.d + sl.o_rows); a.joins = (const int4*)(sl.d + sl.o_joins); a.entries = sl.d + sl.o_entries;
+  a.n_items = sl.n_items; a.n_joins = sl.n_joins;
+  a.seq_m = mt.seq_m; a.seq_p0 = mt.seq_p0; a.block_table = mt.block_table;
+  a.pos_add = pos_add; a.rep = c.n_q_heads / c.n_kv_heads; a.Hkv = c.n_kv_heads; a.layer = layer; a.n_pages = s->n_pages; a.pps = s->pps;
+  a.part_o = s->part_o; a.part_ml = s->part_ml;
+  return a;
 }
 
 // Behind the last layer of a context-build pass only some rows have a reader: those that end a prompt, and the last 512-row piece that the
@@ -655,7 +749,7 @@ static void run_layers(ee_session* s, int l0, int l1, const CallPlan& p, const C
   }
   AttnScratch scr;
   const AttnPlan attn = attention_plan(s, p, pos_add, scr);
-  s->last_attn = m->bf16 ? attn.kind : -1;
+  s->last_attn = !m->bf16 ? -1 : p.shared ? ATTN_SHARED : attn.kind;
   for (int l = l0; l < l1; ++l) {
     const LayerLoc& L = m->L[l];
     const float* g1 = (const float*)(m->base + L.g1);
@@ -687,6 +781,10 @@ static void run_layers(ee_session* s, int l0, int l1, const CallPlan& p, const C
                     bf16_attention(st, plan, q, (const bf16_t*)s->kv, tail->mt, pos_add, s->B, tail->p.max_m, tail->p.total_qt,
                                    Hq, Hkv, D, l, s->n_pages, s->pps, few, (bf16_t*)s->AO, L.o.ktiles()));
         R = rows;
+      } else if (p.shared) {
+        SharedCall a = shared_call(s, *p.shared, mt, pos_add, l);
+        a.q = (const bf16_t*)s->Qb; a.total_qt = p.total_qt; a.out = (bf16_t*)s->AO; a.out_ktiles = L.o.ktiles();
+        KF(KF_ATTN, k_shared_attention(st, a, D));
       } else {
         KF(KF_ATTN, bf16_attention(st, attn, (const bf16_t*)s->Qb, (const bf16_t*)s->kv, mt, pos_add, s->B, p.max_m, p.total_qt,
                                    Hq, Hkv, D, l, s->n_pages, s->pps, scr, (bf16_t*)s->AO, L.o.ktiles()));
@@ -712,8 +810,8 @@ static void run_layers(ee_session* s, int l0, int l1, const CallPlan& p, const C
       o.Y = (float*)s->Qb; o.cs = s->cs; o.rowinfo = s->rowinfo; o.Hq = Hq; o.Hkv = Hkv; o.D = D; o.layer = l; o.n_pages = s->n_pages;
       o.kv = (float*)s->kv;
       KF(KF_GEMM_QKV, f32_qkv(st, s->X, g1, c.rms_eps, Wqkv, M, d, o));
-      KF(KF_ATTN, f32_attention(st, (const float*)s->Qb, (const float*)s->kv, mt, pos_add, M, Hq, Hkv, D, l, s->n_pages, s->pps,
-                                s->max_ctx, (float*)s->AO));
+      KF(KF_ATTN, f32_attention(st, (const float*)s->Qb, Hq * D, (const float*)s->kv, mt, pos_add, M, Hq, Hkv, D, l, s->n_pages, s->pps,
+                                s->max_ctx, (float*)s->AO, Hq * D));
       KF(KF_GEMM_O, f32_gemm(st, (const float*)s->AO, Hq * D, nullptr, 0.f, Wo, s->X, d, M, d, Hq * D, true));
       KF(KF_GEMM_GU, f32_gate_up(st, s->X, g2, c.rms_eps, Wgu, (float*)s->H, M, c.d_ffn, d));
       KF(KF_GEMM_DOWN, f32_gemm(st, (const float*)s->H, c.d_ffn, nullptr, 0.f, Wd, s->X, d, M, d, c.d_ffn, true, end ? sink.rows : nullptr,
@@ -790,7 +888,7 @@ static void exit_head(ee_session* s, int M, int which, int row0 = 0, const int* 
 static int finish(ee_session* s) {
   HIP_TRY(hipGetLastError());
   HIP_TRY(hipStreamSynchronize(s->st));
-  for (int i = 0; i < 2; ++i) s->slot[i].in_flight = false;
+  for (int i = 0; i < 2; ++i) s->slot[i].in_flight = s->shared[i].in_flight = false;
   return EE_OK;
 }
 
@@ -1016,6 +1114,7 @@ extern "C" int ee_seq_release(ee_session* s, int seq) {
   while (!q.pages.empty()) { drop_page(s, q.pages.back()); q.pages.pop_back(); }
   q = SeqState();
   forget_tokens(s, seq, 0);
+  s->attend_ready = false;
   return EE_OK;
 }
 
@@ -1048,6 +1147,7 @@ extern "C" int ee_decode_ar(ee_session* s, int n, int32_t* out) {
   }
   EE_TRY(build_meta(s, 0, p, [&](int b, int, int& tok, int&, int&) { tok = s->seq[b].C.back(); }));
   EE_TRY(upload_meta(s, 0));
+  EE_TRY(share_attention(s, 0, p, n));
   CallMeta mt = meta_ptrs(s, s->slot[0].d);
   std::vector<int> seen(s->B);
   for (int b = 0; b < s->B; ++b) seen[b] = p.p0[b] + 1;
@@ -1135,6 +1235,7 @@ static int draft_impl(ee_session* s, int k, int32_t* draft, const float* u) {
   }, u ? s->B * s->max_rows : 0));
   if (u) put_uniforms(s, p, u, k, nullptr);
   EE_TRY(upload_meta(s, 0));
+  EE_TRY(share_attention(s, 0, p, rows));
   CallMeta mt = meta_ptrs(s, s->slot[0].d);
   std::vector<int> seen(s->B);
   for (int b = 0; b < s->B; ++b) seen[b] = p.p0[b] + 1;
@@ -1200,6 +1301,7 @@ extern "C" int ee_draft_inject(ee_session* s, int k, const int32_t* draft) {
     dst = b * s->max_rows + r;
   }));
   EE_TRY(upload_meta(s, 0));
+  EE_TRY(share_attention(s, 0, p, 1));
   CallMeta mt = meta_ptrs(s, s->slot[0].d);
   PassSource from_tokens; from_tokens.tok = mt.row_tok;
   PassSink keep; keep.rows = s->Hd; keep.row_idx = mt.row_dst;
@@ -1272,7 +1374,7 @@ static int place_scratch_static(ee_session* s, const CallPlan& p) {
   AttnScratch scr;
   const int nsplit = attention_plan(s, p, 0, scr).nsplit;
   Carver cv{base};
-  const size_t slots = (size_t)p.total_qt * c.n_kv_heads * nsplit;
+  const size_t slots = (size_t)c.n_kv_heads * (p.shared ? p.shared->slots : p.total_qt * nsplit);
   float* part_o = cv.take<float>(slots * 16 * c.head_dim);
   float* part_ml = cv.take<float>(slots * 32);
   const size_t pstride = (size_t)ceil_div(p.M, 16) * 16;
@@ -1336,6 +1438,7 @@ static int verify_intermediate_impl(ee_session* s, int32_t* n_accept, int32_t* n
     dst = b * s->max_rows + (int)s->seq[b].V.size() + r;     // H_i row
   }, rs ? s->B * s->max_rows + s->B : 0));
   if (rs) put_uniforms(s, p, u_acc, u_stride, u_res);
+  EE_TRY(share_attention(s, 0, p, 1));
   if (static_scratch) EE_TRY(place_scratch_static(s, p));
   int* h = s->slot[0].h;
   for (int b = 0; b < s->B; ++b) {
@@ -1478,6 +1581,7 @@ static int verify_upper_impl(ee_session* s, int level, const uint8_t* active, in
       dst = b * s->max_rows + m_src[b];
     }));
     EE_TRY(upload_meta(s, 1));
+    EE_TRY(share_attention(s, 1, p, 1));
     CallMeta mt = meta_ptrs(s, s->slot[1].d);
     PassSource from_tokens; from_tokens.tok = mt.row_tok;
     PassSink keep; keep.rows = rows_below; keep.row_idx = mt.row_dst;
@@ -1501,6 +1605,7 @@ static int verify_upper_impl(ee_session* s, int level, const uint8_t* active, in
     for (int i = 0; i < m_src[b]; ++i) h[s->o_cand + (size_t)b * s->cand_stride + i] = src_tok(b, i);
   }
   EE_TRY(upload_meta(s, 0));
+  EE_TRY(share_attention(s, 0, p, 1));
   CallMeta mt = meta_ptrs(s, s->slot[0].d);
   PassSource kept; kept.rows = rows_below; kept.row_idx = mt.row_src;  // consume the buffered rows
   PassSink keep;
@@ -1591,6 +1696,66 @@ extern "C" int ee_sampling_attach(ee_session* s, void* dev_arena, size_t arena_b
   const size_t store = rows * s->m->cfg.vocab;
   s->Pd = f; s->Pi = f + store;
   for (int j = 2; j < s->n_levels; ++j) s->Pup[j - 2] = f + (size_t)j * store;
+  return EE_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// C ABI: attention of given rows over the cache
+// ---------------------------------------------------------------------------------------------
+extern "C" int ee_attend_begin(ee_session* s, const int32_t* rows, const int32_t* pos0) {
+  if (!s || !rows) { ee_set_error("null argument"); return EE_ERR_ARG; }
+  CallPlan p;
+  p.m.assign(s->B, 0); p.p0.assign(s->B, 0);
+  std::vector<int> end(s->B, 0);
+  int any = 0;
+  for (int b = 0; b < s->B; ++b) {
+    if (rows[b] < 0 || rows[b] > s->max_rows) { ee_set_error("sequence %d: %d rows do not fit max_rows %d", b, rows[b], s->max_rows); return EE_ERR_ARG; }
+    if (!rows[b]) continue;
+    const SeqState& q = s->seq[b];
+    if (!q.started) { ee_set_error("sequence %d has no context", b); return EE_ERR_STATE; }
+    const int held = q.len[0], from = pos0 ? pos0[b] : held - rows[b];
+    if (from < 0 || from > held - rows[b]) { ee_set_error("sequence %d: rows at %d..%d, the cache holds %d positions", b, from, from + rows[b] - 1, held); return EE_ERR_ARG; }
+    p.m[b] = rows[b]; p.p0[b] = from;
+    end[b] = from + rows[b];
+    any++;
+  }
+  if (!any) { ee_set_error("no query rows are given"); return EE_ERR_ARG; }
+  EE_TRY(build_meta(s, 0, p, [](int, int, int&, int&, int&) {}, 0, false));
+  EE_TRY(upload_meta(s, 0));
+  EE_TRY(share_attention(s, 0, p, 1, true));
+  HIP_TRY(hipGetLastError());
+  s->attend = p;
+  s->attend_end = end;
+  s->attend_ready = true;
+  return EE_OK;
+}
+
+extern "C" int ee_attend(ee_session* s, int layer, const void* q, int dtype, int64_t q_stride, void* out, int64_t out_stride) {
+  if (!s || !q || !out) { ee_set_error("null argument"); return EE_ERR_ARG; }
+  const ee_config& c = s->m->cfg;
+  if (!s->attend_ready) { ee_set_error("no rows are fixed (ee_attend_begin), or the session moved on since"); return EE_ERR_STATE; }
+  if (layer < 0 || layer >= c.n_layers) { ee_set_error("layer out of range"); return EE_ERR_ARG; }
+  if (dtype != c.dtype) { ee_set_error("q and out are of the model's dtype"); return EE_ERR_ARG; }
+  const int width = c.n_q_heads * c.head_dim;
+  if (q_stride < width || out_stride < width) { ee_set_error("row strides must be at least %d", width); return EE_ERR_ARG; }
+  const int unit = s->m->bf16 ? 16 : 4;
+  if (((uintptr_t)q | (uintptr_t)out) % unit || (s->m->bf16 && (q_stride % 8 || out_stride % 8))) { ee_set_error("q and out must be 16-byte aligned, row by row"); return EE_ERR_ARG; }
+  if (q == out) { ee_set_error("out may not be q"); return EE_ERR_ARG; }
+  int g = 0;
+  while (layer >= s->m->exits[g]) ++g;
+  for (int b = 0; b < s->B; ++b)
+    if (s->attend_end[b] > s->seq[b].len[g]) { ee_set_error("layer %d holds %d positions of sequence %d", layer, s->seq[b].len[g], b); return EE_ERR_ARG; }
+  const CallMeta mt = meta_ptrs(s, s->slot[0].d);
+  if (s->m->bf16) {
+    SharedCall a = shared_call(s, *s->attend.shared, mt, 0, layer);
+    a.by_rows = true;
+    a.q = (const bf16_t*)q; a.q_stride = q_stride; a.out = (bf16_t*)out; a.out_stride = out_stride;
+    k_shared_attention(s->st, a, c.head_dim);
+  } else {
+    f32_attention(s->st, (const float*)q, q_stride, (const float*)s->kv, mt, 0, s->attend.M, c.n_q_heads, c.n_kv_heads, c.head_dim, layer,
+                  s->n_pages, s->pps, s->max_ctx, (float*)out, out_stride);
+  }
+  HIP_TRY(hipGetLastError());
   return EE_OK;
 }
 
@@ -1732,6 +1897,7 @@ extern "C" int kv_rollback(ee_session* s, int seq, int group_mask, int new_len) 
   if (!s || seq < 0 || seq >= s->B) { ee_set_error("bad sequence index"); return EE_ERR_ARG; }
   SeqState& q = s->seq[seq];
   if (!q.started) { ee_set_error("sequence %d has no context", seq); return EE_ERR_STATE; }
+  s->attend_ready = false;
   const int n = s->n_levels;
   const int m12 = group_mask & 3;
   if (m12 != 0 && m12 != 3) { ee_set_error("G1 and G2 roll back together"); return EE_ERR_ARG; }
@@ -1921,6 +2087,11 @@ extern "C" int ee_debug_attention_split_pages(int pages) {
 extern "C" int ee_debug_attention_form(int form) {
   if (form < -1 || form > ATTN_TILE) { ee_set_error("form must be -1 (built-in choice), 0, 1 or 2"); return EE_ERR_ARG; }
   g_attn_form = form;
+  return EE_OK;
+}
+extern "C" int ee_debug_shared_attention(int mode) {
+  if (mode < -1 || mode > 1) { ee_set_error("mode must be -1 (built-in choice), 0 or 1"); return EE_ERR_ARG; }
+  g_shared_attention = mode;
   return EE_OK;
 }
 extern "C" int ee_debug_last_attention(const ee_session* s) { return s ? s->last_attn : -1; }
