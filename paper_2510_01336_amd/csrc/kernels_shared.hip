@@ -44,17 +44,16 @@ __device__ inline void store_out(const SharedCall& a, int row, int head, int kvh
   *(uint2*)p = make_uint2(pack2(x, y), pack2(z, w));
 }
 
-// Workgroup = (KV head, item): up to eight packed q-tiles and a run of pages.  Wave (qg, par) owns tiles 2*qg, 2*qg+1 and every second page; pages
-// reach LDS by direct global->LDS loads, two slots of two pages each, one barrier per pair of pages; the parities of a tile meet in LDS at the
-// end.
+// Workgroup = (KV head, item): up to eight packed q-tiles and a run of pages.  Four waves; wave w owns tiles w and w + 4.  A page reaches LDS by
+// direct global->LDS loads, two slots, one barrier a page; two workgroups share a compute unit, so that one's softmax, start and end run under the
+// other's matrix instructions and loads.
 template <int D, bool ROWS>
-__global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
+__global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
   constexpr int DS = D / 32, DT = D / 16, KCH = 4 * DS, CH = KCH + 2 * DT;     // 1 KiB chunks of a page: K first, then V
-  constexpr int CPW = CH / 4;                                                  // chunks a wave requests per step
-  __shared__ u32x4 lds[4][CH * 64];                                            // slot 2 * (step mod 2) + parity
-  __shared__ float2 ml[4][2][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, qc = lane & 15;
-  const int wave_s = __builtin_amdgcn_readfirstlane(wave), qg = wave_s & 3, par = wave_s >> 2;
+  constexpr int CPW = CH / 4;                                                  // chunks a wave requests per page
+  __shared__ u32x4 lds[2][CH * 64];
+  const int lane = threadIdx.x & 63, g = lane >> 4, qc = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x;
   const int* it = a.items + 8 * blockIdx.y;
   const int tile0 = it[0], n_tiles = it[1], seq = it[2], page0 = it[3], slot0 = it[5];
@@ -66,22 +65,22 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
       *(float2*)(a.part_ml + (((size_t)(slot0 + (threadIdx.x >> 4)) * a.Hkv + kvh) * 16 + (threadIdx.x & 15)) * 2) = make_float2(-INFINITY, 0.f);
     return;
   }
-  const int npg = page1 - page0, nst = (npg + 1) >> 1;
+  const int npg = page1 - page0;
   const int* bt = a.block_table + (size_t)seq * a.pps + page0;
   typedef const __attribute__((address_space(1))) void* gptr_t;
   typedef __attribute__((address_space(3))) void* lptr_t;
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lptr_t)&lds[0][0]);
-  auto request = [&](int step, int page) __attribute__((always_inline)) {
-    const u32x4* src = (const u32x4*)(a.kv + kv_slab(a.layer, page, kvh, a.n_pages, a.Hkv, D)) + qg * CPW * 64 + lane;
-    const unsigned dst = lds0 + 1024u * (((step & 1) * 2 + par) * CH + qg * CPW);
+  auto request = [&](int pg, int page) __attribute__((always_inline)) {
+    const u32x4* src = (const u32x4*)(a.kv + kv_slab(a.layer, page, kvh, a.n_pages, a.Hkv, D)) + wave * CPW * 64 + lane;
+    const unsigned dst = lds0 + 1024u * ((pg & 1) * CH + wave * CPW);
 #pragma unroll
     for (int j = 0; j < CPW; ++j) __builtin_amdgcn_global_load_lds((gptr_t)(src + j * 64), (lptr_t)(size_t)(dst + 1024u * j), 16, 0, 0);
   };
-  request(0, bt[min(par, npg - 1)]);
-  int next_page = bt[min(2 + par, npg - 1)];
+  request(0, bt[0]);
+  int next_page = bt[min(1, npg - 1)];
   // pages before this one are seen whole by every row of the item
-  const int first_masked = own ? (a.rows[tile0 * 16].w + a.pos_add + 1) / EE_PAGE - page0 : npg + 2;
-  bool has[2];
+  const int first_masked = own ? (a.rows[tile0 * 16].w + a.pos_add + 1) / EE_PAGE - page0 : npg;
+  const int nt = (wave < n_tiles) + (wave + 4 < n_tiles);          // tiles of this wave
   int limit[2];
   int4 row[2];
   u32x4 qf[2][DS];
@@ -89,8 +88,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
   f32x4 o[2][DT], lacc[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    has[i] = 2 * qg + i < n_tiles;
-    row[i] = a.rows[(tile0 + (has[i] ? 2 * qg + i : 0)) * 16 + qc];
+    row[i] = a.rows[(tile0 + (i < nt ? wave + 4 * i : 0)) * 16 + qc];
     limit[i] = row[i].x < 0 ? -1 : own ? row[i].w + a.pos_add : INT_MAX;
     const bf16_t* q = q_address<D, ROWS>(a, row[i], kvh, g);
 #pragma unroll
@@ -101,10 +99,11 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
   }
   const float sc2 = 1.4426950408889634f / sqrtf((float)D);         // scores in base-2 units
   const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-  auto page_step = [&](auto masked_c, const u32x4* L, int pg) __attribute__((always_inline)) {
+  auto page_step = [&](auto tiles_c, auto masked_c, const u32x4* L, int pg) __attribute__((always_inline)) {
+    constexpr int NT = decltype(tiles_c)::value;
     constexpr bool MASKED = decltype(masked_c)::value;
     const int base = (page0 + pg) * EE_PAGE + 16 * g;  // this lane group holds positions base .. base+15
-    f32x4 s4[2][4];
+    f32x4 s4[NT][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {                      // (fragments in halves: 256 registers hold no more)
       u32x4 kf[2 * DS];
@@ -113,21 +112,21 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) s4[i][2 * h + t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < NT; ++i) s4[i][2 * h + t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < DS; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) s4[i][2 * h + t] = mfma16(kf[t * DS + s], qf[i][s], s4[i][2 * h + t]);
+          for (int i = 0; i < NT; ++i) s4[i][2 * h + t] = mfma16(kf[t * DS + s], qf[i][s], s4[i][2 * h + t]);
       __builtin_amdgcn_sched_barrier(0);
     }
     u32x4 vf[DT];                                      // first half of V, requested under the softmax
 #pragma unroll
     for (int c = 0; c < DT; ++c) vf[c] = L[(KCH + c) * 64];
-    u32x4 P[2][2];
+    u32x4 P[NT][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NT; ++i) {
       float tmax = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -163,7 +162,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
         for (int c = 0; c < DT; ++c) vf[c] = L[(KCH + DT + c) * 64];
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) lacc[i] = mfma16(ones, P[i][h], lacc[i]);
+      for (int i = 0; i < NT; ++i) lacc[i] = mfma16(ones, P[i][h], lacc[i]);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -177,68 +176,50 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(SharedCall a) {
             }
           }
 #pragma unroll
-          for (int i = 0; i < 2; ++i) o[i][h * DT / 2 + dt] = mfma16(v, P[i][ks], o[i][h * DT / 2 + dt]);
+          for (int i = 0; i < NT; ++i) o[i][h * DT / 2 + dt] = mfma16(v, P[i][ks], o[i][h * DT / 2 + dt]);
         }
     }
   };
-  auto open_step = [&](int st) __attribute__((always_inline)) {
-    // own requests of this step landed; behind the barrier everybody's, and everybody is done with the other two slots
+  auto open_step = [&](int pg) __attribute__((always_inline)) {
+    // own requests of this page landed; behind the barrier everybody's, and everybody is done with the other slot
     __builtin_amdgcn_s_waitcnt(0x70);                  // vmcnt(0) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (st + 1 < nst) {
-      request(st + 1, next_page);
-      next_page = bt[min(2 * (st + 2) + par, npg - 1)];
+    if (pg + 1 < npg) {
+      request(pg + 1, next_page);
+      next_page = bt[min(pg + 2, npg - 1)];
     }
-    return &lds[0][0] + ((st & 1) * 2 + par) * (CH * 64) + lane;
+    return &lds[pg & 1][0] + lane;
   };
-  int st = 0;
-  for (; 2 * st + 1 < first_masked && 2 * st + 1 < npg; ++st) {
-    const u32x4* L = open_step(st);
-    if (has[0]) page_step(std::false_type{}, L, 2 * st + par);
+  using one = std::integral_constant<int, 1>;
+  using two = std::integral_constant<int, 2>;
+  int pg = 0;
+  for (; pg < min(first_masked, npg); ++pg) {
+    const u32x4* L = open_step(pg);
+    if (nt == 2) page_step(two{}, std::false_type{}, L, pg);
+    else if (nt == 1) page_step(one{}, std::false_type{}, L, pg);
   }
-  for (; st < nst; ++st) {
-    const u32x4* L = open_step(st);
-    if (has[0] && 2 * st + par < npg) page_step(std::true_type{}, L, 2 * st + par);
+  for (; pg < npg; ++pg) {
+    const u32x4* L = open_step(pg);
+    if (nt == 2) page_step(two{}, std::true_type{}, L, pg);
+    else if (nt == 1) page_step(one{}, std::true_type{}, L, pg);
   }
-  // the odd pages' partials through LDS to the waves of the even pages
-  __syncthreads();
-  f32x4* po = (f32x4*)&lds[0][0] + qg * (2 * DT * 64) + lane;
-  if (par == 1 && has[0]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      ml[qg][i][lane] = make_float2(mrun[i], lacc[i][0]);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) po[(i * DT + dt) * 64] = o[i][dt];
-    }
-  }
-  __syncthreads();
-  if (par == 1) return;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (!has[i]) continue;
-    const float2 t = ml[qg][i][lane];
-    const float mm = fmaxf(mrun[i], t.x), ms = mm == -INFINITY ? 0.f : mm;
-    const float f0 = __builtin_amdgcn_exp2f(mrun[i] - ms), f1 = __builtin_amdgcn_exp2f(t.x - ms);
-    const float l = lacc[i][0] * f0 + t.y * f1;
+    if (i >= nt) break;
+    const float l = lacc[i][0];
     if (slot0 < 0) {
       if (row[i].x < 0) continue;
-      const float inv = 1.0f / l, a0 = f0 * inv, a1 = f1 * inv;
+      const float inv = 1.0f / l;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const f32x4 x = po[(i * DT + dt) * 64];
-        store_out<D, ROWS>(a, row[i].x, row[i].y, kvh, dt * 16 + 4 * g, o[i][dt][0] * a0 + x[0] * a1, o[i][dt][1] * a0 + x[1] * a1,
-                           o[i][dt][2] * a0 + x[2] * a1, o[i][dt][3] * a0 + x[3] * a1);
-      }
+      for (int dt = 0; dt < DT; ++dt)
+        store_out<D, ROWS>(a, row[i].x, row[i].y, kvh, dt * 16 + 4 * g, o[i][dt][0] * inv, o[i][dt][1] * inv, o[i][dt][2] * inv, o[i][dt][3] * inv);
     } else {
-      const size_t at = ((size_t)(slot0 + 2 * qg + i) * a.Hkv + kvh) * 16 + qc;
-      if (g == 0) *(float2*)(a.part_ml + at * 2) = make_float2(mm, l);
+      const size_t at = ((size_t)(slot0 + wave + 4 * i) * a.Hkv + kvh) * 16 + qc;
+      if (g == 0) *(float2*)(a.part_ml + at * 2) = make_float2(mrun[i], l);
       float* p = a.part_o + at * D + 4 * g;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const f32x4 x = po[(i * DT + dt) * 64];
-        *(f32x4*)(p + dt * 16) = f32x4{o[i][dt][0] * f0 + x[0] * f1, o[i][dt][1] * f0 + x[1] * f1, o[i][dt][2] * f0 + x[2] * f1, o[i][dt][3] * f0 + x[3] * f1};
-      }
+      for (int dt = 0; dt < DT; ++dt) *(f32x4*)(p + dt * 16) = o[i][dt];
     }
   }
 }
@@ -287,7 +268,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedCall a) {
 
 template <int D, bool ROWS>
 static void launch_shared(hipStream_t st, const SharedCall& a) {
-  hipLaunchKernelGGL((shared_attn_kernel<D, ROWS>), dim3(a.Hkv, a.n_items), dim3(512), 0, st, a);
+  hipLaunchKernelGGL((shared_attn_kernel<D, ROWS>), dim3(a.Hkv, a.n_items), dim3(256), 0, st, a);
   if (a.n_joins > 0)
     hipLaunchKernelGGL((shared_join_kernel<D, ROWS>), dim3((unsigned)(((size_t)a.n_joins * a.Hkv + 3) / 4)), dim3(256), 0, st, a);
 }
