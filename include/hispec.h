@@ -430,6 +430,11 @@ int ee_debug_attention_form(int form);
 int ee_debug_last_attention(const ee_session* s);
 int ee_debug_shared_attention(int mode);
 
+/* Test support, process-wide: how often ee_logit_rules looks for a missing piece of a row (a microsecond or so each) before it leaves the piece's
+ * scaling to a launch of its own; 0: every piece at once, -1 restores the built-in count.  Results do not depend on it.
+ * EE_ERR_ARG below -1. */
+int ee_debug_rules_looks(int looks);
+
 /* Plain device-to-device streaming copy on `stream` (pointers and size multiples of 16 bytes; not
  * synchronised).  A kernel of exactly known traffic -- `bytes` read, `bytes` written -- used to
  * calibrate hardware byte counters when the HBM traffic of the other kernels is measured. */

@@ -22,7 +22,7 @@ __all__ = [
     "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist", "ee_attend_begin", "ee_attend",
     "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
     "ee_debug_enable_logits", "ee_debug_last_logits", "ee_debug_last_hidden", "ee_debug_read_kv", "ee_debug_write_kv",
-    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_shared_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
+    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_shared_attention", "ee_debug_rules_looks", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
     "EE_F32", "EE_BF16", "TENSOR_IDS", "EXPORTED_SYMBOLS",
 ]
 
@@ -38,7 +38,7 @@ EXPORTED_SYMBOLS = [
     "ee_draft_sample", "ee_verify_intermediate_rs", "ee_verify_full_rs", "ee_verify_level_rs", "ee_debug_read_dist", "ee_attend_begin", "ee_attend",
     "ee_logit_rules_bytes", "ee_logit_rules", "ee_rules_bytes", "ee_rules_attach", "ee_rules_set", "ee_rules_rows", "ee_get_lengths", "ee_get_counts", "ee_get_tokens",
     "ee_debug_enable_logits", "ee_debug_last_logits", "ee_debug_last_hidden", "ee_debug_read_kv", "ee_debug_write_kv",
-    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_shared_attention", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
+    "ee_debug_poison_dead_kv", "ee_debug_time_kernels", "ee_debug_kernel_times", "ee_debug_gemm_row_blocks", "ee_debug_gemm_block_tiles", "ee_debug_attention_split_pages", "ee_debug_attention_form", "ee_debug_last_attention", "ee_debug_shared_attention", "ee_debug_rules_looks", "ee_debug_stream_copy", "ee_debug_read_floor", "ee_last_error",
 ]
 
 
@@ -121,6 +121,7 @@ def _load():
         "ee_attend_begin": (C.c_int, [vp, i32p, i32p]),
         "ee_attend": (C.c_int, [vp, C.c_int, vp, C.c_int, C.c_int64, vp, C.c_int64]),
         "ee_debug_shared_attention": (C.c_int, [C.c_int]),
+        "ee_debug_rules_looks": (C.c_int, [C.c_int]),
         "ee_logit_rules_bytes": (C.c_size_t, [C.c_int, C.c_int]),
         "ee_logit_rules": (C.c_int, [C.POINTER(ee_rules_call), vp]),
         "ee_rules_bytes": (C.c_size_t, [vp, C.c_int]),
@@ -525,6 +526,10 @@ def ee_debug_last_attention(session: int) -> int:
 
 def ee_debug_shared_attention(mode: int) -> None:
     _chk(lib.ee_debug_shared_attention(int(mode)))
+
+
+def ee_debug_rules_looks(looks: int) -> None:
+    _chk(lib.ee_debug_rules_looks(int(looks)))
 
 
 def ee_debug_time_kernels(session: int, on: bool) -> None:

@@ -6,30 +6,39 @@
 //   x <- x + bias;   x <- x / T;   x <- -inf where the row's mask does not allow the token
 //
 // Counts are not state: every launch takes them from the token lists, so a history that shrinks (rejected drafts) costs nothing
-// and nothing has to be undone.  A workgroup owns a piece of the vocabulary for one sequence: it reads the history once, keeps
-// the counts of its piece in LDS (integer adds: the order does not matter), and applies them to all rows of the sequence, adding the
-// one more token that each further row sees.  The softmax takes a second launch where a row has several pieces: the first leaves
-// exp(x - max of the piece) and the piece's (max, sum), the second scales.
+// and nothing has to be undone.  A workgroup owns a piece of one row: its logits go to registers and stay there, the counts of its tokens are
+// gathered in LDS (integer adds: the order does not matter) while they arrive.  The row's pieces meet for the softmax without another pass over
+// memory: each publishes its (max, sum) as one 64-bit word and looks for the others' words, so that a row is read once and written once.  Workgroups
+// start in about the order of their numbers and a row's are neighbours, so the words are there within a microsecond or two; should they not be
+// (another launch holds the compute units), a piece gives up after a while, leaves its exponentials unscaled, and a last launch, which
+// otherwise finds nothing to do, scales them.  So no workgroup waits for one that cannot start.
 #include "kernels.h"
 
 #define EE_RULES_SEEN 0x80000000u        // in the prompt; the lower bits count the tokens behind it
 
 // Each of the five steps rounds to fp32 by itself (no contraction), so that equal inputs tie exactly and a tie goes to the lowest id.
-struct SeqRules { float rep, freq, pres, temp; };
-__device__ inline float rule_penalty(float x, uint32_t w, const SeqRules& q) {
+__device__ inline float rule_penalty(float x, uint32_t w, float rep, float freq, float pres) {
 #pragma clang fp contract(off)
   if (w) {
-    x = x > 0.f ? x / q.rep : x * q.rep;
-    const float c = (float)(w & ~EE_RULES_SEEN), fc = q.freq * c;
+    x = x > 0.f ? x / rep : x * rep;
+    const float c = (float)(w & ~EE_RULES_SEEN), fc = freq * c;
     x = x - fc;
-    if (w & ~EE_RULES_SEEN) x = x - q.pres;
+    if (w & ~EE_RULES_SEEN) x = x - pres;
   }
   return x;
 }
-__device__ inline float rule_finish(float x, float bias, float temp) {
-#pragma clang fp contract(off)
-  x = x + bias;
-  return x / temp;
+// x / t, correctly rounded, from y = 1 / t correctly rounded: two residual steps (the first leaves a quotient within an ulp, from which the second
+// rounds right: Markstein 1990), five instructions where the general division takes eleven and a reciprocal.  The quotient stays as it is where it
+// is not finite.  (Quotients below 2^-100 may be an ulp off.)
+__device__ inline float rule_divide(float x, float t, float y) {
+  const float q0 = x * y, q1 = fmaf(fmaf(-q0, t, x), y, q0), q2 = fmaf(fmaf(-q1, t, x), y, q1);
+  return fabsf(q0) < INFINITY ? q2 : q0;
+}
+// e^x for x <= 0 (-inf: 0): the hardware's power of two, the rounding of its argument made good to first order; within 2^-22 of the value
+__device__ inline float rule_exp(float x) {
+  x = fmaxf(x, -200.f);
+  const float t = x * 1.44269502f, lo = fmaf(x, 1.44269502f, -t) + x * 1.92596299e-8f, e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, lo * 0.693147182f, e);
 }
 
 template <int T>
@@ -68,269 +77,366 @@ __device__ inline int rules_block_min(int v, float* sh) {
   return v;
 }
 
-struct RulesWork { float *pmax, *psum; int* pidx; int pieces, groups; bool vec; };
+// slots: a word per (row, piece) -- softmax: the piece's max and sum; arg max alone: max and token.  Of softmaxes of several pieces: late, per (row, piece)
+// 0, or 1 + the piece's token of the highest logit where it was left unscaled; n_late: how many; looks: when to give up
+struct RulesWork { unsigned long long* slots; unsigned *late, *n_late; int pieces, looks; };
+#define EE_RULES_EMPTY 0xffffffffffffffffull      // (no published word: sums are not negative, NaN has another pattern)
 
-// T threads, 4 R tokens each: pieces of 4 T R tokens.  blockIdx.x = piece + pieces * sequence, blockIdx.y = share of the
-// sequence's rows.
-template <int T, int R, bool BIAS>
-__global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep step, RulesWork wk) {
-  constexpr int C = 4 * T * R;
-  __shared__ uint32_t cnt[C];
-  __shared__ int bidx[BIAS ? C : 4];
-  __shared__ float red[T / 64];
-  const int piece = blockIdx.x % wk.pieces, b = blockIdx.x / wk.pieces, tid = threadIdx.x;
-  const int r0 = min(max(a.row_start[b], 0), a.rows), r1 = min(max(a.row_start[b + 1], 0), a.rows);
-  const int m = r1 - r0, share = (m + wk.groups - 1) / max(1, wk.groups);
-  const int i0 = blockIdx.y * share, i1 = min(m, i0 + share);
-  if (i0 >= i1) return;                                       // whole workgroup
-  const int c0 = piece * C, cn = min(C, a.vocab - c0);        // this piece's tokens
-  const bool hist = a.tokens != nullptr;
-  SeqRules q;
-  q.rep = a.repetition ? a.repetition[b] : 1.f;
-  q.freq = a.frequency ? a.frequency[b] : 0.f;
-  q.pres = a.presence ? a.presence[b] : 0.f;
-  q.temp = a.temperature ? a.temperature[b] : 1.f;
-  const int* tok = hist ? a.tokens + (size_t)b * a.tokens_stride : nullptr;
-  const int cap = a.tokens_room;
-  const int n0 = hist ? max(0, a.first_len[b]) + step.add : 0, np = hist && a.prompt_len ? a.prompt_len[b] : 0;
-  // index i of the history: the list itself, but for the token that the step before drew, which is on its way into the list
-  const int held = step.last ? n0 - 1 : -1;
-  const int late = step.last && r0 < a.rows ? step.last[r0] : -1;
-  auto count = [&](int token, int at) {
-    const unsigned x = (unsigned)(token - c0);
-    if (x < (unsigned)cn) {
-      if (at < np) atomicOr(&cnt[x], EE_RULES_SEEN); else atomicAdd(&cnt[x], 1u);
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));            // rows may start at any element
+typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
+
+// A row from its pieces' words, by one wave (lane l reads those of pieces l, l + 64, ...; sums in a fixed order): max, sum, first piece that holds the
+// max (0 if none does); whole: all words are there, after at most so many further looks.
+struct RulesRow { float mx, sum; int winner; bool whole; };
+__device__ inline RulesRow rules_collect(const unsigned long long* words, int pieces, int looks) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, sum = 0.f;
+  int winner = 0x7fffffff;
+  bool missing = false;
+  for (int k = lane; k < pieces; k += 64) {
+    unsigned long long w = __hip_atomic_load(words + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (; w == EE_RULES_EMPTY && looks > 0; --looks) {
+      __builtin_amdgcn_s_sleep(1);
+      w = __hip_atomic_load(words + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-  };
-  if (hist) {
-    for (int k = 4 * tid; k < C; k += 4 * T) *(uint4*)(cnt + k) = make_uint4(0, 0, 0, 0);
+    missing |= w == EE_RULES_EMPTY;
+    const float mk = __uint_as_float((unsigned)(w >> 32)), sk = __uint_as_float((unsigned)w);
+    if (mk > m) { sum *= rule_exp(m - mk); m = mk; winner = k; }
+    if (mk > -INFINITY) sum += sk * rule_exp(mk - m);
   }
-  if (BIAS)
-    for (int k = 4 * tid; k < C; k += 4 * T) *(int4*)(bidx + k) = make_int4(-1, -1, -1, -1);
-  __syncthreads();
-  if (hist) {
-    const int n = min(n0 + i0, cap);
-    for (int k = tid; k < n; k += 4 * T) {                    // four loads in flight
-      int t[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t[j] = tok[min(k + j * T, n - 1)];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (k + j * T < n) count(k + j * T == held ? late : t[j], k + j * T);
-    }
-    if (step.hist && step.last && piece == 0 && i0 == 0 && tid == 0 && held >= 0 && held < cap) step.hist[(size_t)b * a.tokens_stride + held] = late;
-  }
-  if (BIAS) {
-    const int e0 = min(max(a.bias_start[b], 0), a.n_bias), e1 = min(a.bias_start[b + 1], a.n_bias);
-    for (int e = e0 + tid; e < e1; e += T) {
-      const unsigned x = (unsigned)(a.bias_token[e] - c0);
-      if (x < (unsigned)cn) atomicMax(&bidx[x], e);           // (a token listed twice: the last entry counts)
-    }
-  }
-  __syncthreads();
-  for (int i = i0; i < i1; ++i) {
-    const int r = r0 + i;
-    if (hist && i > i0) {                                     // one more token than the row before
-      __syncthreads();
-      const int at = n0 + i - 1;
-      if (tid == 0 && at < cap) count(tok[at], at);
-      __syncthreads();
-    }
-    const uint32_t* mask = nullptr;
-    if (a.allowed) {
-      const int mr = a.allowed_row ? a.allowed_row[(size_t)step.add * a.rows + r] : r;
-      if (mr >= 0 && mr < a.allowed_rows) mask = a.allowed + (size_t)mr * a.allowed_stride;
-    }
-    const size_t in0 = (size_t)r * a.logits_stride + c0, out0 = (size_t)r * a.out_stride + c0;
-    float v[R][4];
-    float mx = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int x = 4 * (tid + k * T);
-      if (wk.vec && x + 3 < cn) {
-        if (a.dtype == EE_F32) {
-          const float4 f = *(const float4*)((const float*)a.logits + in0 + x);
-          v[k][0] = f.x; v[k][1] = f.y; v[k][2] = f.z; v[k][3] = f.w;
-        } else {
-          const uint2 f = *(const uint2*)((const bf16_t*)a.logits + in0 + x);
-          v[k][0] = __uint_as_float(f.x << 16); v[k][1] = __uint_as_float(f.x & 0xffff0000u);
-          v[k][2] = __uint_as_float(f.y << 16); v[k][3] = __uint_as_float(f.y & 0xffff0000u);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[k][e] = x + e < cn ? (a.dtype == EE_F32 ? ((const float*)a.logits)[in0 + x + e] : bf16_to_f32(((const bf16_t*)a.logits)[in0 + x + e])) : -INFINITY;
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int x = 4 * (tid + k * T);
-      uint32_t w[4] = {0, 0, 0, 0};
-      int bi[4] = {-1, -1, -1, -1};
-      if (hist) { const uint4 c4 = *(const uint4*)(cnt + x); w[0] = c4.x; w[1] = c4.y; w[2] = c4.z; w[3] = c4.w; }
-      if (BIAS) { const int4 b4 = *(const int4*)(bidx + x); bi[0] = b4.x; bi[1] = b4.y; bi[2] = b4.z; bi[3] = b4.w; }
-      uint32_t ok = 15u;
-      if (mask) ok = x < cn ? (mask[(c0 + x) >> 5] >> ((c0 + x) & 31)) & 15u : 0u;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float y = rule_penalty(v[k][e], w[e], q);
-        y = rule_finish(y, BIAS && bi[e] >= 0 ? a.bias_value[bi[e]] : 0.f, q.temp);
-        v[k][e] = ((ok >> e) & 1u) && x + e < cn ? y : -INFINITY;
-        mx = fmaxf(mx, v[k][e]);
-      }
-    }
-    auto store = [&]() {
-#pragma unroll
-      for (int k = 0; k < R; ++k) {
-        const int x = 4 * (tid + k * T);
-        if (wk.vec && x + 3 < cn) *(float4*)(a.out + out0 + x) = make_float4(v[k][0], v[k][1], v[k][2], v[k][3]);
-        else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) if (x + e < cn) a.out[out0 + x + e] = v[k][e];
-        }
-      }
-    };
-    if (!a.probs) store();
-    if (!a.probs && !a.argmax) continue;
-    mx = rules_block_max<T>(mx, red);
-    const size_t slot = (size_t)r * wk.pieces + piece;
-    if (a.argmax) {
-      int first = 0x7fffffff;
-#pragma unroll
-      for (int k = R - 1; k >= 0; --k)
-#pragma unroll
-        for (int e = 3; e >= 0; --e)
-          if (v[k][e] == mx && mx > -INFINITY) first = c0 + 4 * (tid + k * T) + e;
-      first = rules_block_min<T>(first, red);
-      if (tid == 0) {
-        if (wk.pieces == 1) {
-          const int id = mx > -INFINITY ? first : -1;
-          a.argmax[r] = id;
-          take_token(step.take, r, id);
-        } else {
-          wk.pidx[slot] = first;
-        }
-      }
-    }
-    if (a.probs) {
-      const float safe = mx > -INFINITY ? mx : 0.f;
-      float s = 0.f;
-#pragma unroll
-      for (int k = 0; k < R; ++k) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[k][e] = expf(v[k][e] - safe);
-        s += (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]);
-      }
-      s = rules_block_sum<T>(s, red);
-      if (wk.pieces == 1) {
-        const float inv = s > 0.f ? 1.0f / s : 0.f;
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[k][e] *= inv;
-      } else if (tid == 0) {
-        wk.psum[slot] = s;
-      }
-      store();
-    }
-    if (tid == 0 && wk.pieces > 1) wk.pmax[slot] = mx;
-  }
+  RulesRow row;
+  row.mx = m;
+  for (int d = 1; d < 64; d <<= 1) row.mx = fmaxf(row.mx, __shfl_xor(row.mx, d, 64));
+  sum = m > -INFINITY ? sum * rule_exp(m - row.mx) : 0.f;
+  winner = m == row.mx && m > -INFINITY ? winner : 0x7fffffff;
+  for (int d = 1; d < 64; d <<= 1) { sum += __shfl_xor(sum, d, 64); winner = min(winner, __shfl_xor(winner, d, 64)); }
+  row.sum = sum;
+  row.winner = winner == 0x7fffffff ? 0 : winner;
+  row.whole = __ballot(missing) == 0;
+  return row;
 }
 
-// The rows' pieces join: softmax factors exp(max of the piece - max) / sum on the first launch's exponentials, and the arg max.
-// A workgroup takes `span` tokens of one row (all of one piece).
-__global__ __launch_bounds__(256) void rules_join_kernel(ee_rules_call a, RulesStep step, RulesWork wk, int chunk, int span, int parts) {
-  __shared__ float red[4];
-  const int r = blockIdx.x / parts, part = blockIdx.x % parts, tid = threadIdx.x;
-  if (r < min(max(a.row_start[0], 0), a.rows) || r >= min(a.row_start[a.n_seq], a.rows)) return;      // of no sequence: left as it is
-  const float* pm = wk.pmax + (size_t)r * wk.pieces;
+// T threads, 4 R tokens each: pieces of 4 T R tokens.
+template <int T, int R>
+__global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep step, RulesWork wk) {
+  constexpr int C = 4 * T * R;
+  __shared__ uint32_t tab[C];
+  __shared__ float red[T / 64];
+  __shared__ int s_seq[1];
+  const int tid = threadIdx.x, r = blockIdx.x / (unsigned)wk.pieces, piece = blockIdx.x % (unsigned)wk.pieces;
+  const int c0 = piece * C, cn = min(C, a.vocab - c0);        // this piece's tokens
+  // the row's sequence; the logits are on their way meanwhile
+  const size_t in0 = (size_t)r * a.logits_stride + c0, out0 = (size_t)r * a.out_stride + c0;
+  float v[R][4];
+  if (a.dtype == EE_F32) {
+    const float* x = (const float*)a.logits + in0;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int i = 4 * (tid + k * T);
+      if (i + 3 < cn) {
+        const f32x4u f = *(const f32x4u*)(x + i);
+        v[k][0] = f[0]; v[k][1] = f[1]; v[k][2] = f[2]; v[k][3] = f[3];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[k][e] = i + e < cn ? x[i + e] : 0.f;
+      }
+    }
+  } else {
+    const bf16_t* x = (const bf16_t*)a.logits + in0;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int i = 4 * (tid + k * T);
+      if (i + 3 < cn) {
+        const u32x2u f = *(const u32x2u*)(x + i);
+        v[k][0] = __uint_as_float(f[0] << 16); v[k][1] = __uint_as_float(f[0] & 0xffff0000u);
+        v[k][2] = __uint_as_float(f[1] << 16); v[k][3] = __uint_as_float(f[1] & 0xffff0000u);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[k][e] = i + e < cn ? bf16_to_f32(x[i + e]) : 0.f;
+      }
+    }
+  }
+  const uint32_t* mask = nullptr;
+  if (a.allowed) {
+    const int mr = a.allowed_row ? a.allowed_row[(size_t)step.add * a.rows + r] : r;
+    if (mr >= 0 && mr < a.allowed_rows) mask = a.allowed + (size_t)mr * a.allowed_stride;
+  }
+  uint32_t ok[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const int i = c0 + 4 * (tid + k * T);
+    ok[k] = !mask ? 15u : i < a.vocab ? (mask[i >> 5] >> (i & 31)) & 15u : 0u;
+  }
+  // the row's sequence b: one thread finds row_start[b] <= r < row_start[b + 1] (-1: none)
+  if (tid == 0) s_seq[0] = -1;
+  __syncthreads();
+  for (int b = tid; b < a.n_seq; b += T)
+    if (a.row_start[b] <= r && r < a.row_start[b + 1]) s_seq[0] = b;
+  const bool hist = a.tokens != nullptr;
+  if (hist) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) *(uint4*)(tab + 4 * (tid + k * T)) = make_uint4(0, 0, 0, 0);
+  }
+  __syncthreads();
+  const int b = __builtin_amdgcn_readfirstlane(s_seq[0]);
+  if (b < 0) return;                                          // a row of no sequence (all of its workgroups)
+  const int i0 = r - a.row_start[b];
+  const float temp = a.temperature ? a.temperature[b] : 1.f;
+  const float rep = a.repetition ? a.repetition[b] : 1.f, freq = a.frequency ? a.frequency[b] : 0.f, pres = a.presence ? a.presence[b] : 0.f;
+  const int e0 = a.bias_start ? min(max(a.bias_start[b], 0), a.n_bias) : 0, e1 = a.bias_start ? min(a.bias_start[b + 1], a.n_bias) : 0;
+  if (hist) {
+    const int* tok = a.tokens + (size_t)b * a.tokens_stride;
+    // index i of the history is tok[i], but for the token that the step before took, which is on its way into the list
+    const int cap = a.tokens_room, n0 = max(0, a.first_len[b]) + step.add, n = min(n0 + i0, cap), np = a.prompt_len ? a.prompt_len[b] : 0;
+    const int held = step.last ? n0 - 1 : -1, late = step.last ? step.last[r - i0] : -1;
+    auto count = [&](int token, int at) __attribute__((always_inline)) {
+      const unsigned x = (unsigned)(token - c0);
+      if (at < n && x < (unsigned)cn) {
+        if (at < np) atomicOr(&tab[x], EE_RULES_SEEN); else atomicAdd(&tab[x], 1u);
+      }
+    };
+    const int whole = held >= 0 ? min(n, held) & ~3 : n & ~3; // (groups of four that lie in the list whole)
+    for (int k = 4 * tid; k < whole; k += 16 * T) {           // four loads of four tokens in flight
+      i32x4u t[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) t[j] = *(const i32x4u*)(tok + min(k + j * 4 * T, whole - 4));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k + j * 4 * T < whole)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) count(t[j][e], k + j * 4 * T + e);
+    }
+    if (tid < n - whole) count(whole + tid == held ? late : tok[whole + tid], whole + tid);
+    if (step.hist && step.last && piece == 0 && i0 == 0 && tid == 0 && held >= 0 && held < cap) step.hist[(size_t)b * a.tokens_stride + held] = late;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const uint4 w = *(const uint4*)(tab + 4 * (tid + k * T));
+      if (w.x | w.y | w.z | w.w) {
+        v[k][0] = rule_penalty(v[k][0], w.x, rep, freq, pres); v[k][1] = rule_penalty(v[k][1], w.y, rep, freq, pres);
+        v[k][2] = rule_penalty(v[k][2], w.z, rep, freq, pres); v[k][3] = rule_penalty(v[k][3], w.w, rep, freq, pres);
+      }
+    }
+  }
+  if (e0 < e1) {                                              // the same table again: 1 + the last entry of every token
+#pragma unroll
+    for (int k = 0; k < R; ++k) *(uint4*)(tab + 4 * (tid + k * T)) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    for (int e = e0 + tid; e < e1; e += T) {
+      const unsigned x = (unsigned)(a.bias_token[e] - c0);
+      if (x < (unsigned)cn) atomicMax(&tab[x], (unsigned)e + 1u);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const uint4 w = *(const uint4*)(tab + 4 * (tid + k * T));
+      if (w.x | w.y | w.z | w.w) {
+        if (w.x) v[k][0] += a.bias_value[w.x - 1];
+        if (w.y) v[k][1] += a.bias_value[w.y - 1];
+        if (w.z) v[k][2] += a.bias_value[w.z - 1];
+        if (w.w) v[k][3] += a.bias_value[w.w - 1];
+      }
+    }
+  }
+  const float inv_t = 1.0f / temp;
   float mx = -INFINITY;
-  for (int k = tid; k < wk.pieces; k += 256) mx = fmaxf(mx, pm[k]);
-  mx = rules_block_max<256>(mx, red);
-  if (a.argmax && part == 0) {
-    int first = 0x7fffffff;
-    for (int k = tid; k < wk.pieces; k += 256)
-      if (pm[k] == mx && mx > -INFINITY) first = min(first, wk.pidx[(size_t)r * wk.pieces + k]);
-    first = rules_block_min<256>(first, red);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const int i = 4 * (tid + k * T);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float y = temp == 1.f ? v[k][e] : rule_divide(v[k][e], temp, inv_t);
+      v[k][e] = ((ok[k] >> e) & 1u) && i + e < cn ? y : -INFINITY;
+      mx = fmaxf(mx, v[k][e]);
+    }
+  }
+  auto store = [&]() {
+    float* y = a.out + out0;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int i = 4 * (tid + k * T);
+      if (i + 3 < cn) {
+        f32x4u f;
+        f[0] = v[k][0]; f[1] = v[k][1]; f[2] = v[k][2]; f[3] = v[k][3];
+        *(f32x4u*)(y + i) = f;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (i + e < cn) y[i + e] = v[k][e];
+      }
+    }
+  };
+  if (!a.probs) {
+    store();
+    if (!a.argmax) return;
+  }
+  mx = rules_block_max<T>(mx, red);
+  int first = 0x7fffffff;
+  if (a.argmax) {
+#pragma unroll
+    for (int k = R - 1; k >= 0; --k)
+#pragma unroll
+      for (int e = 3; e >= 0; --e)
+        if (v[k][e] == mx && mx > -INFINITY) first = c0 + 4 * (tid + k * T) + e;
+    first = rules_block_min<T>(first, red);
+  }
+  const unsigned long long hi = (unsigned long long)__float_as_uint(mx) << 32;
+  unsigned long long* mine = wk.slots + (size_t)r * wk.pieces;
+  if (!a.probs) {                                             // arg max alone: a second launch reads the words
     if (tid == 0) {
+      if (wk.pieces == 1) {
+        const int id = mx > -INFINITY ? first : -1;
+        a.argmax[r] = id;
+        take_token(step.take, r, id);
+      } else {
+        mine[piece] = hi | (unsigned)first;
+      }
+    }
+    return;
+  }
+  const float safe = mx > -INFINITY ? mx : 0.f;
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[k][e] = rule_exp(v[k][e] - safe);
+    s += (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]);
+  }
+  s = rules_block_sum<T>(s, red);
+  float f = s > 0.f ? 1.0f / s : 0.f;
+  if (wk.pieces == 1) {
+    if (a.argmax && tid == 0) {
       const int id = mx > -INFINITY ? first : -1;
       a.argmax[r] = id;
       take_token(step.take, r, id);
     }
-  }
-  if (!a.probs) return;
-  const float* ps = wk.psum + (size_t)r * wk.pieces;
-  const float safe = mx > -INFINITY ? mx : 0.f;
-  float s = 0.f;
-  for (int k = tid; k < wk.pieces; k += 256) s += ps[k] * expf(pm[k] - safe);
-  s = rules_block_sum<256>(s, red);
-  const int x0 = part * span, xe = min(a.vocab, x0 + span), piece = x0 / chunk;
-  const float f = s > 0.f ? expf(pm[piece] - safe) / s : 0.f;
-  float* y = a.out + (size_t)r * a.out_stride;
-  if (wk.vec) {
-#pragma unroll 4
-    for (int x = x0 + 4 * tid; x < xe; x += 1024) {
-      if (x + 3 < xe) {
-        float4 t = *(float4*)(y + x);
-        t.x *= f; t.y *= f; t.z *= f; t.w *= f;
-        *(float4*)(y + x) = t;
-      } else {
-        for (int e = 0; e < 4; ++e) if (x + e < xe) y[x + e] *= f;
+  } else {
+    if (tid < 64) {                                           // publish, then look for the row's words
+      if (tid == 0) __hip_atomic_store(mine + piece, hi | __float_as_uint(s), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const RulesRow row = rules_collect(mine, wk.pieces, wk.looks);
+      if (tid == 0) {
+        red[0] = !row.whole ? 1.f : mx > -INFINITY ? rule_exp(mx - row.mx) / row.sum : 0.f;
+        if (!row.whole) {
+          wk.late[(size_t)r * wk.pieces + piece] = 1u + (unsigned)first;
+          atomicAdd(wk.n_late, 1u);
+        } else if (a.argmax && row.winner == piece) {
+          const int id = row.mx > -INFINITY ? first : -1;
+          a.argmax[r] = id;
+          take_token(step.take, r, id);
+        }
       }
     }
-  } else {
-    for (int x = x0 + tid; x < xe; x += 256) y[x] *= f;
+    __syncthreads();
+    f = red[0];
+  }
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[k][e] *= f;
+  store();
+}
+
+// in front of a softmax of several pieces: nothing published, nothing late
+__global__ __launch_bounds__(256) void rules_clear_kernel(RulesWork wk, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) { wk.slots[i] = EE_RULES_EMPTY; wk.late[i] = 0u; }
+  if (i == 0) *wk.n_late = 0u;
+}
+// behind it: the pieces that gave up (none as a rule; C tokens each)
+__global__ __launch_bounds__(256) void rules_late_kernel(ee_rules_call a, RulesStep step, RulesWork wk, int C, int n) {
+  if (*wk.n_late == 0) return;
+  __shared__ float red[1];
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const unsigned mark = wk.late[i];
+    if (mark == 0) continue;                                  // (the whole workgroup)
+    const int r = i / wk.pieces, piece = i % wk.pieces;
+    if (threadIdx.x < 64) {
+      const RulesRow row = rules_collect(wk.slots + (size_t)r * wk.pieces, wk.pieces, 0);
+      if (threadIdx.x == 0) {
+        const float mx = __uint_as_float((unsigned)(wk.slots[i] >> 32));
+        red[0] = mx > -INFINITY ? rule_exp(mx - row.mx) / row.sum : 0.f;
+        if (a.argmax && row.winner == piece) {
+          const int id = row.mx > -INFINITY ? (int)(mark - 1u) : -1;
+          a.argmax[r] = id;
+          take_token(step.take, r, id);
+        }
+      }
+    }
+    __syncthreads();
+    const float f = red[0];
+    float* y = a.out + (size_t)r * a.out_stride;
+    for (int x = piece * C + (int)threadIdx.x; x < min(a.vocab, (piece + 1) * C); x += 256) y[x] *= f;
+    __syncthreads();
+  }
+}
+// the arg max of a row of several pieces: a wave per row
+__global__ __launch_bounds__(256) void rules_argmax_kernel(ee_rules_call a, RulesStep step, RulesWork wk) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (r >= a.rows || r < a.row_start[0] || r >= a.row_start[a.n_seq]) return;      // (whole wave; rows of no sequence are left as they are)
+  float m = -INFINITY;
+  int first = 0x7fffffff;
+  for (int k = lane; k < wk.pieces; k += 64) {
+    const unsigned long long w = wk.slots[(size_t)r * wk.pieces + k];
+    const float mk = __uint_as_float((unsigned)(w >> 32));
+    if (mk > m) { m = mk; first = (int)(unsigned)w; }          // (pieces in order: of equals the first)
+  }
+  for (int d = 1; d < 64; d <<= 1) {
+    const float om = __shfl_xor(m, d, 64);
+    const int of = __shfl_xor(first, d, 64);
+    if (om > m || (om == m && of < first)) { m = om; first = of; }
+  }
+  if (lane == 0) {
+    const int id = m > -INFINITY ? first : -1;
+    a.argmax[r] = id;
+    take_token(step.take, r, id);
   }
 }
 
 // ---- launch shapes ----
-struct RulesShape { int chunk, groups; };
-static const int kRulesChunks[] = {1024, 4096, 8192, 16384, 32768};
-// Pieces as long as the launch still has two workgroups per compute unit: a longer piece reads the history less often.  Where
-// sequences have several rows these are shared out before the pieces are cut below 4096 tokens.
-static RulesShape rules_shape(int rows, int n_seq, int vocab, bool bias) {
-  const int per_seq = max(1, ceil_div(rows, max(1, n_seq)));
-  RulesShape s{1024, 1};
-  for (int c : kRulesChunks) {
-    if (bias && c > 16384) break;
-    s.chunk = c;
-    if (c >= vocab || (long)ceil_div(vocab, 2 * c) * n_seq < 512) break;
+static const int kRulesPieces[] = {1024, 2048, 4096, 8192, 16384};
+// The longest piece of which the launch still has two workgroups per compute unit (a longer piece reads the history and meets its row less often), or
+// the shortest that covers the vocabulary.
+static int rules_piece(int rows, int vocab) {
+  int piece = kRulesPieces[0];
+  for (int c : kRulesPieces) {
+    if (c != piece && (long)ceil_div(vocab, c) * rows < 512) break;
+    piece = c;
+    if (c >= vocab) break;
   }
-  const long wgs = (long)ceil_div(vocab, s.chunk) * n_seq;
-  if (wgs < 512) s.groups = (int)min((long)per_seq, (512 + wgs - 1) / wgs);
-  return s;
+  return piece;
 }
-static size_t rules_slots(int rows, int vocab) { return (size_t)rows * ceil_div(vocab, kRulesChunks[0]); }
-size_t k_rules_workspace(int rows, int vocab) { return (rules_slots(rows, vocab) * 3 * sizeof(float) + 255) / 256 * 256; }
+static size_t rules_words(int rows, int vocab) { return (size_t)rows * ceil_div(vocab, kRulesPieces[0]); }
+size_t k_rules_workspace(int rows, int vocab) { return (rules_words(rows, vocab) * (sizeof(unsigned long long) + sizeof(unsigned)) + 256 + 255) / 256 * 256; }
+static const int kRulesLooks = 1 << 12;
+static int g_rules_looks = kRulesLooks;  // at a missing word, a microsecond or so each (test hook: 0 leaves every piece that meets none to the last launch)
+extern "C" int ee_debug_rules_looks(int looks) {
+  if (looks < -1) { ee_set_error("looks must be -1 (built-in) or more"); return EE_ERR_ARG; }
+  g_rules_looks = looks < 0 ? kRulesLooks : looks;
+  return EE_OK;
+}
 
 void k_rules(hipStream_t st, const ee_rules_call& a, const RulesStep& step) {
   if (a.rows <= 0 || a.n_seq <= 0) return;
-  const bool bias = a.bias_start != nullptr;
-  const RulesShape sh = rules_shape(a.rows, a.n_seq, a.vocab, bias);
+  const int piece = rules_piece(a.rows, a.vocab);
   RulesWork wk;
-  const size_t slots = rules_slots(a.rows, a.vocab);
-  wk.pmax = (float*)a.workspace; wk.psum = wk.pmax + slots; wk.pidx = (int*)(wk.psum + slots);
-  wk.pieces = ceil_div(a.vocab, sh.chunk); wk.groups = sh.groups;
-  const int es = a.dtype == EE_F32 ? 4 : 2;
-  wk.vec = a.logits_stride % 4 == 0 && a.out_stride % 4 == 0 && (uintptr_t)a.logits % (4 * es) == 0 && (uintptr_t)a.out % 16 == 0;
-  const dim3 grid((unsigned)wk.pieces * a.n_seq, sh.groups);
-#define RULES_LAUNCH(T_, R_)                                                                            \
-  do {                                                                                                  \
-    if (bias) hipLaunchKernelGGL((rules_kernel<T_, R_, true>), grid, dim3(T_), 0, st, a, step, wk);     \
-    else hipLaunchKernelGGL((rules_kernel<T_, R_, false>), grid, dim3(T_), 0, st, a, step, wk);         \
-  } while (0)
-  switch (sh.chunk) {
-    case 1024: RULES_LAUNCH(256, 1); break;
-    case 4096: RULES_LAUNCH(256, 4); break;
-    case 8192: RULES_LAUNCH(512, 4); break;
-    case 16384: RULES_LAUNCH(1024, 4); break;
-    default: hipLaunchKernelGGL((rules_kernel<1024, 8, false>), grid, dim3(1024), 0, st, a, step, wk);
+  wk.pieces = ceil_div(a.vocab, piece);
+  wk.slots = (unsigned long long*)((char*)a.workspace + 256);
+  wk.late = (unsigned*)(wk.slots + rules_words(a.rows, a.vocab));
+  wk.n_late = (unsigned*)a.workspace;
+  wk.looks = g_rules_looks;
+  const int words = wk.pieces * a.rows;
+  const bool meet = a.probs && wk.pieces > 1;
+  if (meet) hipLaunchKernelGGL(rules_clear_kernel, dim3(ceil_div(words, 256)), dim3(256), 0, st, wk, words);
+  switch (piece) {
+    case 1024: hipLaunchKernelGGL((rules_kernel<256, 1>), dim3(words), dim3(256), 0, st, a, step, wk); break;
+    case 2048: hipLaunchKernelGGL((rules_kernel<256, 2>), dim3(words), dim3(256), 0, st, a, step, wk); break;
+    case 4096: hipLaunchKernelGGL((rules_kernel<256, 4>), dim3(words), dim3(256), 0, st, a, step, wk); break;
+    case 8192: hipLaunchKernelGGL((rules_kernel<512, 4>), dim3(words), dim3(512), 0, st, a, step, wk); break;
+    default: hipLaunchKernelGGL((rules_kernel<512, 8>), dim3(words), dim3(512), 0, st, a, step, wk);
   }
-#undef RULES_LAUNCH
-  if (wk.pieces > 1 && (a.probs || a.argmax)) {
-    const int span = a.probs ? min(sh.chunk, 4096) : a.vocab, parts = a.probs ? ceil_div(a.vocab, span) : 1;
-    hipLaunchKernelGGL(rules_join_kernel, dim3((unsigned)parts * a.rows), dim3(256), 0, st, a, step, wk, sh.chunk, span, parts);
-  }
+  if (meet) hipLaunchKernelGGL(rules_late_kernel, dim3(min(words, 256)), dim3(256), 0, st, a, step, wk, piece, words);
+  if (!a.probs && a.argmax && wk.pieces > 1)
+    hipLaunchKernelGGL(rules_argmax_kernel, dim3(ceil_div(a.rows, 4)), dim3(256), 0, st, a, step, wk);
 }
 
 // What a call uploads, read from page-locked host memory: its small tables (workgroup 0), the new ends of the token lists (workgroup 1 + b).
@@ -383,7 +489,7 @@ extern "C" int ee_logit_rules(const ee_rules_call* c, void* stream) {
   if (!a.workspace || (uintptr_t)a.workspace & 255 || a.workspace_bytes < k_rules_workspace(a.rows, a.vocab)) {
     ee_set_error("logit rules: workspace must be 256-byte aligned and of ee_logit_rules_bytes()"); return EE_ERR_ARG;
   }
-  if ((long)ceil_div(a.vocab, kRulesChunks[0]) * max(a.rows, a.n_seq) > 0x7fffffffL) { ee_set_error("logit rules: too many rows"); return EE_ERR_ARG; }
+  if ((long)ceil_div(a.vocab, kRulesPieces[0]) * a.rows > 0x7fffffffL) { ee_set_error("logit rules: too many rows"); return EE_ERR_ARG; }
   k_rules((hipStream_t)stream, a, RulesStep());
   HIP_TRY(hipGetLastError());
   return EE_OK;

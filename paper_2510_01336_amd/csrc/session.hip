@@ -467,7 +467,7 @@ static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool a
     q[b].n_pages = ceil_div(p.p0[b] + p.m[b] + steps - 1, EE_PAGE);
     q[b].pages = s->seq[b].pages.data();
   }
-  const int wgs = std::max(1, 256 / s->m->cfg.n_kv_heads);
+  const int wgs = std::max(1, 512 / s->m->cfg.n_kv_heads);      // (two workgroups a compute unit)
   SharedPlan P = plan_shared(q, rep, (int)s->part_units, wgs, 2, true);
   SharedSlot& sl = s->shared[si];
   auto fits = [&](const SharedPlan& x) {

@@ -8,6 +8,7 @@
 #pragma once
 #include <algorithm>
 #include <climits>
+#include <functional>
 #include <vector>
 
 struct SharedSeq {            // one sequence of the call (m == 0: not taking part)
@@ -80,8 +81,8 @@ inline void shared_segments(const std::vector<SharedSeq>& q, const std::vector<i
   }
 }
 
-// Cost of an item in microseconds on a compute unit, and of a slot's partial results, by measurement (shared_attn_kernel).
-inline double shared_item_us(int tiles, int pages) { return 4.0 + pages * (0.45 + 0.1 * std::max(2, tiles)); }
+// Cost of an item in microseconds on its half of a compute unit, by measurement (shared_attn_kernel).
+inline double shared_item_us(int tiles, int pages) { return 4.5 + pages * (0.8 + 0.25 * tiles); }
 
 // rep: query heads per KV head; most_slots: room for partial results; wgs: items of one KV head that run at a time; least: pages of
 // a shared segment at the least; share: false keeps every sequence to itself; per_forced > 0: pages per item.
@@ -113,41 +114,62 @@ inline SharedPlan plan_shared(const std::vector<SharedSeq>& q, int rep, int most
     P.shares |= s.seqs.size() > 1;
     P.pages_read += (long)(s.page1 - s.page0) * ((at.back().tiles + block - 1) / block);
   }
-  // pages per item: the cheapest schedule by the model (rounds of items over the compute units, and the partial results)
-  int longest = 1;
-  for (const SharedSegment& s : segs) longest = std::max(longest, s.page1 - s.page0);
-  auto schedule = [&](int per, double& us) {
-    double work = 0, most = 0;
+  // Pages per item, of shared segments and of the sequences' own: the pair whose items, dealt in their order to whichever of `wgs` places is free first,
+  // are done soonest, the joining of the partial results counted in.
+  int longest[2] = {1, 1};                              // shared, own
+  for (const SharedSegment& s : segs) longest[s.own] = std::max(longest[s.own], s.page1 - s.page0);
+  std::vector<double> free_at;
+  auto schedule = [&](const int* per, double& us) {
     long slots = 0;
-    for (size_t i = 0; i < segs.size(); ++i) {
-      const auto [cuts, run] = shared_cuts(segs[i].page1 - segs[i].page0, per);
-      for (int t = 0; t < at[i].tiles; t += block) {
-        const double c = shared_item_us(std::min(block, at[i].tiles - t), run);
-        work += c * cuts; most = std::max(most, c);
+    free_at.assign(wgs, 0.0);
+    double end = 0;
+    for (int own = 0; own < 2; ++own)
+      for (size_t i = 0; i < segs.size(); ++i) {
+        if (segs[i].own != (own == 1)) continue;
+        const int n = segs[i].page1 - segs[i].page0;
+        const auto [cuts, run] = shared_cuts(n, per[own]);
+        slots += (long)at[i].tiles * cuts;
+        for (int c = 0; c < cuts; ++c)
+          for (int t = 0; t < at[i].tiles; t += block) {
+            std::pop_heap(free_at.begin(), free_at.end(), std::greater<double>());
+            double& f = free_at.back();
+            f += shared_item_us(std::min(block, at[i].tiles - t), std::min(run, n - c * run));
+            end = std::max(end, f);
+            std::push_heap(free_at.begin(), free_at.end(), std::greater<double>());
+          }
       }
-      slots += (long)at[i].tiles * cuts;
-    }
-    us = std::max(most, work / wgs + most / 2) + 0.011 * slots;
+    us = end + 0.012 * slots;
     return slots <= most_slots;
   };
-  int per = longest;
-  double best = 1e30;
-  for (int cuts = 1; cuts <= longest; cuts = cuts < 64 ? cuts + 1 : cuts + cuts / 8) {
-    const int c = (longest + cuts - 1) / cuts;
-    double us = 0;
-    if (!schedule(c, us)) continue;
-    if (us < best) { best = us; per = c; }
-  }
+  int per[2] = {longest[0], longest[1]};
   if (per_forced > 0) {
     double us = 0;
-    per = per_forced;
-    while (per < longest && !schedule(per, us)) ++per;
+    per[0] = per[1] = per_forced;
+    while ((per[0] < longest[0] || per[1] < longest[1]) && !schedule(per, us)) { per[0]++; per[1]++; }
+  } else {
+    double best = 1e30;
+    auto tries = [](int n, int most) {                  // numbers of items of the longest segment, finer where they are few
+      std::vector<int> c;
+      for (int k = 1; k <= std::min(n, most); k += 1 + k / 6) c.push_back((n + k - 1) / k);
+      return c;
+    };
+    for (int own : tries(longest[1], 8))
+      for (int joint : P.shares ? tries(longest[0], wgs) : std::vector<int>{1}) {
+        const int p[2] = {joint, own};
+        double us = 0;
+        if (schedule(p, us) && us < best) { best = us; per[0] = joint; per[1] = own; }
+      }
   }
+#ifdef SP_PROBE
+  if (getenv("SP_S")) per[0] = std::max(1, (longest[0] + atoi(getenv("SP_S")) - 1) / atoi(getenv("SP_S")));
+  if (getenv("SP_O")) per[1] = std::max(1, (longest[1] + atoi(getenv("SP_O")) - 1) / atoi(getenv("SP_O")));
+  { double us = 0; schedule(per, us); static int said = 0; if (said++ < 1 || getenv("SP_SAY")) fprintf(stderr, "plan: per %d %d of %d %d, items of %zu segments, model %.1f us\n", per[0], per[1], longest[0], longest[1], segs.size(), us); }
+#endif
   // items: the cuts of a segment one after the other, all its blocks of a cut together, so that workgroups that run at the same time read the same pages
   std::vector<int> slot_of;                             // per segment: first slot
   std::vector<int> cuts_of(segs.size());
   for (size_t i = 0; i < segs.size(); ++i) {
-    cuts_of[i] = shared_cuts(segs[i].page1 - segs[i].page0, per).cuts;
+    cuts_of[i] = shared_cuts(segs[i].page1 - segs[i].page0, per[segs[i].own]).cuts;
     bool final = cuts_of[i] == 1;
     for (int r = at[i].tile0 * 16; final && r < (at[i].tile0 + at[i].tiles) * 16; ++r)
       final = P.rows[r].row < 0 || parts[(size_t)P.rows[r].row * rep + P.rows[r].head] == 1;
@@ -157,7 +179,7 @@ inline SharedPlan plan_shared(const std::vector<SharedSeq>& q, int rep, int most
   for (int pass = 0; pass < 2; ++pass)                  // shared segments first: their items are the long ones
     for (size_t i = 0; i < segs.size(); ++i) {
       if (segs[i].own != (pass == 1)) continue;
-      const auto [cuts, run] = shared_cuts(segs[i].page1 - segs[i].page0, per);
+      const auto [cuts, run] = shared_cuts(segs[i].page1 - segs[i].page0, per[segs[i].own]);
       for (int c = 0; c < cuts; ++c)
         for (int t = 0; t < at[i].tiles; t += block)
           P.items.push_back({at[i].tile0 + t, std::min(block, at[i].tiles - t), segs[i].seqs[0], segs[i].page0 + c * run,

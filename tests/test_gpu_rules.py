@@ -227,6 +227,24 @@ def test_other_streams_and_two_calls_at_once():
     assert all(torch.equal(want, g) for g in got)
 
 
+def test_pieces_that_do_not_meet_are_scaled_afterwards():
+    """With no wait for the other pieces of a row most pieces are left to the last launch: the same bits, arg max included."""
+    rng = np.random.default_rng(12)
+    for m, vocab in (([1], 128256), ([9, 0, 9], 32003), ([1] * 100, 50000)):
+        p = make(rng, m, vocab, 100, True, 5, True, empty=(2,) if sum(m) > 6 else ())
+        x, rules = torch.from_numpy(p["x"]).cuda(), device_rules(p)
+        want = rules.probs(x, argmax=True)
+        try:
+            hs.ee_debug_rules_looks(0)
+            for _ in range(3):
+                got = rules.probs(x, argmax=True)
+                assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        finally:
+            hs.ee_debug_rules_looks(-1)
+    with pytest.raises(hs.EEError):
+        hs.ee_debug_rules_looks(-2)
+
+
 def test_binding_refuses():
     start = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
     rules = hs.LogitRules(100, start)
