@@ -78,7 +78,8 @@ __device__ inline int rules_block_min(int v, float* sh) {
 }
 
 // slots: a word per (row, piece) -- softmax: the piece's max and sum; arg max alone: max and token.  Of softmaxes of several pieces: late, per (row, piece)
-// 0, or 1 + the piece's token of the highest logit where it was left unscaled; n_late: how many; looks: when to give up
+// 0, or 1 + the piece's token of the highest logit where it was left unscaled; n_late: how many; looks: when to give up (-1: no piece looks, all are late
+// and nothing is cleared or counted)
 struct RulesWork { unsigned long long* slots; unsigned *late, *n_late; int pieces, looks; };
 #define EE_RULES_EMPTY 0xffffffffffffffffull      // (no published word: sums are not negative, NaN has another pattern)
 
@@ -165,8 +166,9 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
   uint32_t ok[R];
 #pragma unroll
   for (int k = 0; k < R; ++k) {
-    const int i = c0 + 4 * (tid + k * T);
-    ok[k] = !mask ? 15u : i < a.vocab ? (mask[i >> 5] >> (i & 31)) & 15u : 0u;
+    const int i = 4 * (tid + k * T);
+    ok[k] = i + 4 <= cn ? 15u : i < cn ? (1u << (cn - i)) - 1u : 0u;
+    if (mask && i < cn) ok[k] &= mask[(c0 + i) >> 5] >> ((c0 + i) & 31);
   }
   // the row's sequence b: one thread finds row_start[b] <= r < row_start[b + 1] (-1: none)
   if (tid == 0) s_seq[0] = -1;
@@ -239,17 +241,21 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
       }
     }
   }
-  const float inv_t = 1.0f / temp;
-  float mx = -INFINITY;
+  if (temp != 1.f) {
+    const float inv_t = 1.0f / temp;
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[k][e] = rule_divide(v[k][e], temp, inv_t);
+  }
+  float own = -INFINITY;                                      // this thread's highest
 #pragma unroll
   for (int k = 0; k < R; ++k) {
-    const int i = 4 * (tid + k * T);
+    if (ok[k] != 15u) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float y = temp == 1.f ? v[k][e] : rule_divide(v[k][e], temp, inv_t);
-      v[k][e] = ((ok[k] >> e) & 1u) && i + e < cn ? y : -INFINITY;
-      mx = fmaxf(mx, v[k][e]);
+      for (int e = 0; e < 4; ++e) v[k][e] = (ok[k] >> e) & 1u ? v[k][e] : -INFINITY;
     }
+    own = fmaxf(own, fmaxf(fmaxf(v[k][0], v[k][1]), fmaxf(v[k][2], v[k][3])));
   }
   auto store = [&]() {
     float* y = a.out + out0;
@@ -270,14 +276,16 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
     store();
     if (!a.argmax) return;
   }
-  mx = rules_block_max<T>(mx, red);
+  const float mx = rules_block_max<T>(own, red);
   int first = 0x7fffffff;
   if (a.argmax) {
+    if (own == mx && mx > -INFINITY) {
 #pragma unroll
-    for (int k = R - 1; k >= 0; --k)
+      for (int k = R - 1; k >= 0; --k)
 #pragma unroll
-      for (int e = 3; e >= 0; --e)
-        if (v[k][e] == mx && mx > -INFINITY) first = c0 + 4 * (tid + k * T) + e;
+        for (int e = 3; e >= 0; --e)
+          if (v[k][e] == mx) first = c0 + 4 * (tid + k * T) + e;
+    }
     first = rules_block_min<T>(first, red);
   }
   const unsigned long long hi = (unsigned long long)__float_as_uint(mx) << 32;
@@ -313,12 +321,14 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
   } else {
     if (tid < 64) {                                           // publish, then look for the row's words
       if (tid == 0) __hip_atomic_store(mine + piece, hi | __float_as_uint(s), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const RulesRow row = rules_collect(mine, wk.pieces, wk.looks);
+      RulesRow row;
+      row.whole = false;
+      if (wk.looks >= 0) row = rules_collect(mine, wk.pieces, wk.looks);
       if (tid == 0) {
         red[0] = !row.whole ? 1.f : mx > -INFINITY ? rule_exp(mx - row.mx) / row.sum : 0.f;
         if (!row.whole) {
           wk.late[(size_t)r * wk.pieces + piece] = 1u + (unsigned)first;
-          atomicAdd(wk.n_late, 1u);
+          if (wk.looks >= 0) atomicAdd(wk.n_late, 1u);
         } else if (a.argmax && row.winner == piece) {
           const int id = row.mx > -INFINITY ? first : -1;
           a.argmax[r] = id;
@@ -342,14 +352,15 @@ __global__ __launch_bounds__(256) void rules_clear_kernel(RulesWork wk, int n) {
   if (i < n) { wk.slots[i] = EE_RULES_EMPTY; wk.late[i] = 0u; }
   if (i == 0) *wk.n_late = 0u;
 }
-// behind it: the pieces that gave up (none as a rule; C tokens each)
+// behind it: the pieces of C tokens that are late (none as a rule, or all)
 __global__ __launch_bounds__(256) void rules_late_kernel(ee_rules_call a, RulesStep step, RulesWork wk, int C, int n) {
-  if (*wk.n_late == 0) return;
+  if (wk.looks >= 0 && *wk.n_late == 0) return;
   __shared__ float red[1];
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const unsigned mark = wk.late[i];
-    if (mark == 0) continue;                                  // (the whole workgroup)
     const int r = i / wk.pieces, piece = i % wk.pieces;
+    if (r < a.row_start[0] || r >= a.row_start[a.n_seq]) continue;      // (the whole workgroup; of no sequence: left as it is)
+    const unsigned mark = wk.late[i];
+    if (mark == 0) continue;
     if (threadIdx.x < 64) {
       const RulesRow row = rules_collect(wk.slots + (size_t)r * wk.pieces, wk.pieces, 0);
       if (threadIdx.x == 0) {
@@ -365,7 +376,14 @@ __global__ __launch_bounds__(256) void rules_late_kernel(ee_rules_call a, RulesS
     __syncthreads();
     const float f = red[0];
     float* y = a.out + (size_t)r * a.out_stride;
-    for (int x = piece * C + (int)threadIdx.x; x < min(a.vocab, (piece + 1) * C); x += 256) y[x] *= f;
+    const int end = min(a.vocab, (piece + 1) * C), quads = piece * C + (end - piece * C) / 4 * 4;
+#pragma unroll 4
+    for (int x = piece * C + 4 * (int)threadIdx.x; x < quads; x += 1024) {
+      f32x4u t = *(const f32x4u*)(y + x);
+      t *= f;
+      *(f32x4u*)(y + x) = t;
+    }
+    if (quads + (int)threadIdx.x < end) y[quads + threadIdx.x] *= f;
     __syncthreads();
   }
 }
@@ -393,9 +411,10 @@ __global__ __launch_bounds__(256) void rules_argmax_kernel(ee_rules_call a, Rule
 }
 
 // ---- launch shapes ----
-static const int kRulesPieces[] = {1024, 2048, 4096, 8192, 16384};
-// The longest piece of which the launch still has two workgroups per compute unit (a longer piece reads the history and meets its row less often), or
-// the shortest that covers the vocabulary.
+static const int kRulesPieces[] = {1024, 2048, 4096, 8192};
+// The longest piece of which the launch still has two workgroups per compute unit (a longer piece reads the history and meets its row less often; beyond 8192 tokens,
+// by 512 threads, nothing is gained: 144 rows of 128256 tokens 53 us, in pieces of 16384 62, of 4096 55, of 2048 by 256 threads 82), or the shortest
+// that covers the vocabulary.
 static int rules_piece(int rows, int vocab) {
   int piece = kRulesPieces[0];
   for (int c : kRulesPieces) {
@@ -415,6 +434,7 @@ extern "C" int ee_debug_rules_looks(int looks) {
   return EE_OK;
 }
 
+static const long kRulesMeet = 2L << 20;               // values of a call beyond which the pieces meet
 void k_rules(hipStream_t st, const ee_rules_call& a, const RulesStep& step) {
   if (a.rows <= 0 || a.n_seq <= 0) return;
   const int piece = rules_piece(a.rows, a.vocab);
@@ -425,16 +445,17 @@ void k_rules(hipStream_t st, const ee_rules_call& a, const RulesStep& step) {
   wk.n_late = (unsigned*)a.workspace;
   wk.looks = g_rules_looks;
   const int words = wk.pieces * a.rows;
-  const bool meet = a.probs && wk.pieces > 1;
+  // A small softmax takes a second pass instead of the meeting (one row of 128256 tokens 13.7 us a call, meeting 18.6: a launch more)
+  const bool joined = a.probs && wk.pieces > 1, meet = joined && (long)a.rows * a.vocab > kRulesMeet;
+  if (joined && !meet) wk.looks = -1;
   if (meet) hipLaunchKernelGGL(rules_clear_kernel, dim3(ceil_div(words, 256)), dim3(256), 0, st, wk, words);
   switch (piece) {
     case 1024: hipLaunchKernelGGL((rules_kernel<256, 1>), dim3(words), dim3(256), 0, st, a, step, wk); break;
     case 2048: hipLaunchKernelGGL((rules_kernel<256, 2>), dim3(words), dim3(256), 0, st, a, step, wk); break;
     case 4096: hipLaunchKernelGGL((rules_kernel<256, 4>), dim3(words), dim3(256), 0, st, a, step, wk); break;
-    case 8192: hipLaunchKernelGGL((rules_kernel<512, 4>), dim3(words), dim3(512), 0, st, a, step, wk); break;
-    default: hipLaunchKernelGGL((rules_kernel<512, 8>), dim3(words), dim3(512), 0, st, a, step, wk);
+    default: hipLaunchKernelGGL((rules_kernel<512, 4>), dim3(words), dim3(512), 0, st, a, step, wk);
   }
-  if (meet) hipLaunchKernelGGL(rules_late_kernel, dim3(min(words, 256)), dim3(256), 0, st, a, step, wk, piece, words);
+  if (joined) hipLaunchKernelGGL(rules_late_kernel, dim3(meet ? min(words, 256) : words), dim3(256), 0, st, a, step, wk, piece, words);
   if (!a.probs && a.argmax && wk.pieces > 1)
     hipLaunchKernelGGL(rules_argmax_kernel, dim3(ceil_div(a.rows, 4)), dim3(256), 0, st, a, step, wk);
 }
