@@ -204,6 +204,18 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+def _raw_stream(index: int) -> int:
+    """torch's current stream of a device (without the Stream object, which costs more than a launch)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
 def _arena(nbytes: int):
     import torch
     t = torch.empty(int(nbytes) + 256, dtype=torch.uint8, device="cuda")
@@ -682,6 +694,7 @@ class Session:
         self.nbytes = arena_bytes or ee_session_bytes(model.handle, batch, max_ctx, max_rows, total_pages)
         self._buf, ptr = _arena(self.nbytes)
         self._hidden, self._logits = _ResultBlocks(), _ResultBlocks()
+        self._attend_form = ((0, 0, 0), None, EE_F32, 0, self._buf.get_device())        # no rows yet
         self.handle = ee_session_create(model.handle, batch, max_ctx, max_rows, total_pages, ptr, self.nbytes, model.stream)
 
     def prefill(self, prompts: Sequence[np.ndarray]) -> np.ndarray:
@@ -709,36 +722,44 @@ class Session:
         """Fix the query rows of the attend calls that follow: rows[b] of sequence b, at positions pos0[b] .. (default: its last ones)."""
         if len(rows) != self.batch or (pos0 is not None and len(pos0) != self.batch):
             raise ValueError(f"an entry for each of {self.batch} sequences")
+        import torch
         ee_attend_begin(self.handle, rows, pos0)
-        self._attend_rows = int(sum(rows))
+        cfg = self.model.cfg
+        bf16 = cfg.dtype == "bf16"
+        self._attend_form = ((int(sum(rows)), cfg.n_q_heads, cfg.head_dim), torch.bfloat16 if bf16 else torch.float32, EE_BF16 if bf16 else EE_F32,
+                             cfg.n_q_heads * cfg.head_dim, self._buf.get_device())
 
     def attend(self, layer: int, q, out=None):
         """Attention of the rows q [rows, query heads, head_dim] (the model's dtype) over one layer of the cache; out: of the same shape.
         Ordered with torch's current stream of the device."""
         import torch
-        cfg = self.model.cfg
-        dt = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
-        shape = (getattr(self, "_attend_rows", 0), cfg.n_q_heads, cfg.head_dim)
+        shape, dt, kind, width, index = self._attend_form
         if out is None:
             out = torch.empty(shape, dtype=dt, device=self._buf.device)
-        for name, t in (("q", q), ("out", out)):
-            if not torch.is_tensor(t) or t.dtype != dt or tuple(t.shape) != shape or t.device != self._buf.device:
-                raise ValueError(f"{name}: a {dt} tensor {list(shape)} on {self._buf.device}")
-            if t.stride(2) != 1 or (t.stride(1) != cfg.head_dim and cfg.n_q_heads > 1):
-                raise ValueError(f"{name}: the heads of a row side by side")
-        width = cfg.n_q_heads * cfg.head_dim
-        qs, os_ = (t.stride(0) if shape[0] > 1 else width for t in (q, out))
-        cur = torch.cuda.current_stream(q.device)
-        args = (self.handle, layer, q.data_ptr(), EE_BF16 if dt == torch.bfloat16 else EE_F32, qs, out.data_ptr(), os_)
-        if cur.cuda_stream == self.model.stream and torch.cuda.current_device() == q.device.index:
-            ee_attend(*args)
+        else:
+            self._check_rows("out", out)
+        self._check_rows("q", q)
+        qs, os_ = (q.stride(0), out.stride(0)) if shape[0] > 1 else (width, width)
+        mine, cur = self.model.stream, _raw_stream(index)
+        if cur == mine and _current_device() == index:
+            ee_attend(self.handle, layer, q.data_ptr(), kind, qs, out.data_ptr(), os_)
             return out
-        with torch.cuda.device(q.device):
-            mine = torch.cuda.ExternalStream(self.model.stream) if self.model.stream else torch.cuda.default_stream(q.device)
-            mine.wait_stream(cur)
-            ee_attend(*args)
-            cur.wait_stream(mine)
+        with torch.cuda.device(index):
+            there = torch.cuda.ExternalStream(mine) if mine else torch.cuda.default_stream(index)
+            here = torch.cuda.current_stream(index)
+            there.wait_stream(here)
+            ee_attend(self.handle, layer, q.data_ptr(), kind, qs, out.data_ptr(), os_)
+            here.wait_stream(there)
         return out
+
+    def _check_rows(self, name: str, t) -> None:
+        import torch
+        shape, dt, _, width, index = self._attend_form
+        if not torch.is_tensor(t) or t.dtype != dt or t.shape != shape or t.get_device() != index:
+            raise ValueError(f"{name}: a {dt} tensor {list(shape)} on {self._buf.device}")
+        st = t.stride()
+        if st[2] != 1 or (st[1] != shape[2] and shape[1] > 1):
+            raise ValueError(f"{name}: the heads of a row side by side")
 
     def release(self, seq: int) -> None:
         ee_seq_release(self.handle, seq)
@@ -898,6 +919,9 @@ class LogitRules:
         if not torch.is_tensor(row_start) or row_start.dim() != 1 or row_start.numel() < 1:
             raise ValueError("row_start: an int32 tensor [n_seq + 1]")
         self.device, self.n_seq, self.vocab = row_start.device, row_start.numel() - 1, int(vocab)
+        self._index, self._dtypes, self._ready = row_start.get_device(), (torch.float32, torch.bfloat16), {}
+        if self._index < 0:
+            raise ValueError("row_start: on a GPU")
         per_seq = {"first_len", "prompt_len", "repetition", "frequency", "presence", "temperature"}
         c = self.call = ee_rules_call()
         for name, t in given.items():
@@ -929,36 +953,52 @@ class LogitRules:
 
     def _run(self, x, probs: bool, argmax: bool, out):
         import torch
-        if not torch.is_tensor(x) or x.dim() != 2 or x.shape[1] != self.vocab or x.device != self.device or \
-                x.dtype not in (torch.float32, torch.bfloat16):
+        if not torch.is_tensor(x) or x.dim() != 2 or x.get_device() != self._index or x.dtype not in self._dtypes or x.shape[1] != self.vocab:
             raise ValueError(f"logits: float32 or bfloat16 [rows, {self.vocab}] on {self.device}")
         rows = x.shape[0]
-        if self._rows is not None and self._rows < rows:
-            raise ValueError(f"allowed_row: an entry for each of {rows} rows")
-        if self.vocab > 1 and x.stride(1) != 1:
+        kind = (rows, x.dtype, probs, argmax)
+        ready = self._ready.get(kind)
+        if ready is None:
+            ready = self._ready[kind] = self._prepare(*kind)
+        call, nbytes = ready
+        c = ee_rules_call.from_buffer_copy(call)
+        if x.stride(1) != 1 and self.vocab > 1:
             raise ValueError("logits: the tokens of a row side by side")
         if out is None:
             out = torch.empty((rows, self.vocab), dtype=torch.float32, device=self.device)
-        elif not torch.is_tensor(out) or out.dtype != torch.float32 or out.shape != x.shape or out.device != self.device or \
-                (self.vocab > 1 and out.stride(1) != 1):
-            raise ValueError("out: float32 of the logits' shape, the tokens of a row side by side")
-        token = torch.empty(rows, dtype=torch.int32, device=self.device) if argmax else None
-        if rows == 0:
-            return (out, token) if argmax else out
-        work = torch.empty(ee_logit_rules_bytes(rows, self.vocab), dtype=torch.uint8, device=self.device)
-        c = ee_rules_call.from_buffer_copy(self.call)
-        c.rows, c.dtype, c.probs = rows, EE_F32 if x.dtype == torch.float32 else EE_BF16, int(probs)
-        c.logits, c.logits_stride = x.data_ptr(), x.stride(0) if rows > 1 else self.vocab
-        c.out, c.out_stride = out.data_ptr(), out.stride(0) if rows > 1 else self.vocab
-        c.argmax = token.data_ptr() if argmax else None
-        off = (-work.data_ptr()) % 256
-        c.workspace, c.workspace_bytes = work.data_ptr() + off, work.numel() - off
-        if torch.cuda.current_device() == self.device.index:
-            ee_logit_rules(c, torch.cuda.current_stream(self.device).cuda_stream)
         else:
-            with torch.cuda.device(self.device):
-                ee_logit_rules(c, torch.cuda.current_stream(self.device).cuda_stream)
+            if not torch.is_tensor(out) or out.dtype != torch.float32 or out.shape != x.shape or out.get_device() != self._index or \
+                    (self.vocab > 1 and out.stride(1) != 1):
+                raise ValueError("out: float32 of the logits' shape, the tokens of a row side by side")
+            c.out_stride = out.stride(0) if rows > 1 else self.vocab
+        token = torch.empty(rows, dtype=torch.int32, device=self.device) if argmax else None
+        if rows:
+            if rows > 1:
+                c.logits_stride = x.stride(0)
+            c.logits, c.out = x.data_ptr(), out.data_ptr()
+            if argmax:
+                c.argmax = token.data_ptr()
+            work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            at = work.data_ptr()
+            c.workspace = at + -at % 256
+            if _current_device() == self._index:
+                ee_logit_rules(c, _raw_stream(self._index))
+            else:
+                with torch.cuda.device(self._index):
+                    ee_logit_rules(c, _raw_stream(self._index))
         return (out, token) if argmax else out
+
+    def _prepare(self, rows: int, dtype, probs: bool, argmax: bool):
+        """The call of so many rows but for its addresses, and the bytes of its workspace."""
+        import torch
+        if self._rows is not None and self._rows < rows:
+            raise ValueError(f"allowed_row: an entry for each of {rows} rows")
+        c = ee_rules_call.from_buffer_copy(self.call)
+        c.rows, c.dtype, c.probs = rows, EE_F32 if dtype == torch.float32 else EE_BF16, int(probs)
+        c.logits_stride = c.out_stride = self.vocab
+        nbytes = ee_logit_rules_bytes(rows, self.vocab)
+        c.workspace_bytes = nbytes - 256
+        return c, nbytes
 
     def logits(self, x, argmax: bool = False, out=None):
         """The adjusted logits (float32); with argmax also the token of every row (int32, -1 where nothing may follow)."""

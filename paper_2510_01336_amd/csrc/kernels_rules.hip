@@ -17,16 +17,6 @@
 #define EE_RULES_SEEN 0x80000000u        // in the prompt; the lower bits count the tokens behind it
 
 // Each of the five steps rounds to fp32 by itself (no contraction), so that equal inputs tie exactly and a tie goes to the lowest id.
-__device__ inline float rule_penalty(float x, uint32_t w, float rep, float freq, float pres) {
-#pragma clang fp contract(off)
-  if (w) {
-    x = x > 0.f ? x / rep : x * rep;
-    const float c = (float)(w & ~EE_RULES_SEEN), fc = freq * c;
-    x = x - fc;
-    if (w & ~EE_RULES_SEEN) x = x - pres;
-  }
-  return x;
-}
 // x / t, correctly rounded, from y = 1 / t correctly rounded: two residual steps (the first leaves a quotient within an ulp, from which the second
 // rounds right: Markstein 1990), five instructions where the general division takes eleven and a reciprocal.  The quotient stays as it is where it
 // is not finite.  (Quotients below 2^-100 may be an ulp off.)
@@ -34,12 +24,32 @@ __device__ inline float rule_divide(float x, float t, float y) {
   const float q0 = x * y, q1 = fmaf(fmaf(-q0, t, x), y, q0), q2 = fmaf(fmaf(-q1, t, x), y, q1);
   return fabsf(q0) < INFINITY ? q2 : q0;
 }
-// e^x for x <= 0 (-inf: 0): the hardware's power of two, the rounding of its argument made good to first order; within 2^-22 of the value
-__device__ inline float rule_exp(float x) {
-  x = fmaxf(x, -200.f);
-  const float t = x * 1.44269502f, lo = fmaf(x, 1.44269502f, -t) + x * 1.92596299e-8f, e = __builtin_amdgcn_exp2f(t);
+__device__ inline float rule_penalty(float x, uint32_t w, float rep, float inv_rep, float freq, float pres) {
+#pragma clang fp contract(off)
+  if (w) {
+    const float quot = rule_divide(x, rep, inv_rep), prod = x * rep;
+    x = x > 0.f ? quot : prod;
+    const float c = (float)(w & ~EE_RULES_SEEN), fc = freq * c;
+    x = x - fc;
+    if (w & ~EE_RULES_SEEN) x = x - pres;
+  }
+  return x;
+}
+// e^(d / t) for d <= 0 (-inf: 0), from log2(e) / t in two parts: the hardware's power of two, the rounding of its argument made good to first order;
+// within 2^-22 of the value
+struct RuleScale { float t, inv, hi, lo, least; };      // t, 1 / t, log2(e) / t in two parts, where the exponential is 0 for good
+__device__ inline RuleScale rule_scale(float t) {
+  RuleScale r;
+  r.t = t; r.inv = 1.0f / t; r.hi = 1.44269502f * r.inv; r.least = -208.f * t;
+  r.lo = (fmaf(-r.hi, t, 1.44269502f) + 1.92596299e-8f) * r.inv;      // (log2(e) is the sum of the two numbers)
+  return r;
+}
+__device__ inline float rule_exp(float d, const RuleScale& c) {
+  d = fmaxf(d, c.least);
+  const float t = d * c.hi, lo = fmaf(d, c.hi, -t) + d * c.lo, e = __builtin_amdgcn_exp2f(t);
   return fmaf(e, lo * 0.693147182f, e);
 }
+__device__ inline float rule_quotient(float x, const RuleScale& c) { return rule_divide(x, c.t, c.inv); }
 
 template <int T>
 __device__ inline float rules_block_max(float v, float* sh) {
@@ -87,10 +97,11 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));           
 typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
 
-// A row from its pieces' words, by one wave (lane l reads those of pieces l, l + 64, ...; sums in a fixed order): max, sum, first piece that holds the
-// max (0 if none does); whole: all words are there, after at most so many further looks.
+// A row from its pieces' words, by one wave (lane l reads those of pieces l, l + 64, ...; sums in a fixed order): the highest logit in front of the
+// temperature, the sum of the exponentials relative to it, the first piece that holds the highest logit behind the temperature (0 if none does); whole: all words
+// are there, after at most so many further looks.
 struct RulesRow { float mx, sum; int winner; bool whole; };
-__device__ inline RulesRow rules_collect(const unsigned long long* words, int pieces, int looks) {
+__device__ inline RulesRow rules_collect(const unsigned long long* words, int pieces, int looks, const RuleScale& c) {
   const int lane = threadIdx.x & 63;
   float m = -INFINITY, sum = 0.f;
   int winner = 0x7fffffff;
@@ -103,14 +114,18 @@ __device__ inline RulesRow rules_collect(const unsigned long long* words, int pi
     }
     missing |= w == EE_RULES_EMPTY;
     const float mk = __uint_as_float((unsigned)(w >> 32)), sk = __uint_as_float((unsigned)w);
-    if (mk > m) { sum *= rule_exp(m - mk); m = mk; winner = k; }
-    if (mk > -INFINITY) sum += sk * rule_exp(mk - m);
+    if (mk > m) {
+      if (rule_quotient(mk, c) != rule_quotient(m, c)) winner = k;
+      sum *= rule_exp(m - mk, c);
+      m = mk;
+    }
+    if (mk > -INFINITY) sum += sk * rule_exp(mk - m, c);
   }
   RulesRow row;
   row.mx = m;
   for (int d = 1; d < 64; d <<= 1) row.mx = fmaxf(row.mx, __shfl_xor(row.mx, d, 64));
-  sum = m > -INFINITY ? sum * rule_exp(m - row.mx) : 0.f;
-  winner = m == row.mx && m > -INFINITY ? winner : 0x7fffffff;
+  sum = m > -INFINITY ? sum * rule_exp(m - row.mx, c) : 0.f;
+  winner = m > -INFINITY && rule_quotient(m, c) == rule_quotient(row.mx, c) ? winner : 0x7fffffff;
   for (int d = 1; d < 64; d <<= 1) { sum += __shfl_xor(sum, d, 64); winner = min(winner, __shfl_xor(winner, d, 64)); }
   row.sum = sum;
   row.winner = winner == 0x7fffffff ? 0 : winner;
@@ -187,6 +202,7 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
   const float temp = a.temperature ? a.temperature[b] : 1.f;
   const float rep = a.repetition ? a.repetition[b] : 1.f, freq = a.frequency ? a.frequency[b] : 0.f, pres = a.presence ? a.presence[b] : 0.f;
   const int e0 = a.bias_start ? min(max(a.bias_start[b], 0), a.n_bias) : 0, e1 = a.bias_start ? min(a.bias_start[b + 1], a.n_bias) : 0;
+  const int biased = e0 + tid < e1 ? a.bias_token[e0 + tid] : -1;      // (on its way under the history's counts)
   if (hist) {
     const int* tok = a.tokens + (size_t)b * a.tokens_stride;
     // index i of the history is tok[i], but for the token that the step before took, which is on its way into the list
@@ -211,13 +227,14 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
     }
     if (tid < n - whole) count(whole + tid == held ? late : tok[whole + tid], whole + tid);
     if (step.hist && step.last && piece == 0 && i0 == 0 && tid == 0 && held >= 0 && held < cap) step.hist[(size_t)b * a.tokens_stride + held] = late;
+    const float inv_rep = 1.0f / rep;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const uint4 w = *(const uint4*)(tab + 4 * (tid + k * T));
       if (w.x | w.y | w.z | w.w) {
-        v[k][0] = rule_penalty(v[k][0], w.x, rep, freq, pres); v[k][1] = rule_penalty(v[k][1], w.y, rep, freq, pres);
-        v[k][2] = rule_penalty(v[k][2], w.z, rep, freq, pres); v[k][3] = rule_penalty(v[k][3], w.w, rep, freq, pres);
+        v[k][0] = rule_penalty(v[k][0], w.x, rep, inv_rep, freq, pres); v[k][1] = rule_penalty(v[k][1], w.y, rep, inv_rep, freq, pres);
+        v[k][2] = rule_penalty(v[k][2], w.z, rep, inv_rep, freq, pres); v[k][3] = rule_penalty(v[k][3], w.w, rep, inv_rep, freq, pres);
       }
     }
   }
@@ -226,7 +243,7 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
     for (int k = 0; k < R; ++k) *(uint4*)(tab + 4 * (tid + k * T)) = make_uint4(0, 0, 0, 0);
     __syncthreads();
     for (int e = e0 + tid; e < e1; e += T) {
-      const unsigned x = (unsigned)(a.bias_token[e] - c0);
+      const unsigned x = (unsigned)((e == e0 + tid ? biased : a.bias_token[e]) - c0);
       if (x < (unsigned)cn) atomicMax(&tab[x], (unsigned)e + 1u);
     }
     __syncthreads();
@@ -241,7 +258,9 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
       }
     }
   }
-  if (temp != 1.f) {
+  // (the softmax divides inside its exponents; which token is highest is decided by the rounded quotients either way)
+  const RuleScale sc = rule_scale(a.probs ? temp : 1.f);
+  if (!a.probs && temp != 1.f) {
     const float inv_t = 1.0f / temp;
 #pragma unroll
     for (int k = 0; k < R; ++k)
@@ -277,20 +296,19 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
     if (!a.argmax) return;
   }
   const float mx = rules_block_max<T>(own, red);
-  int first = 0x7fffffff;
-  if (a.argmax) {
-    if (own == mx && mx > -INFINITY) {
+  int first = 0x7fffffff;                                     // this thread's first token of the piece's highest logit; the piece's is looked for where it is wanted
+  const float near = mx - (fabsf(mx) * 4.8e-7f + 1e-37f);     // (below it no quotient rounds to that of mx)
+  if (a.argmax && own >= near && mx > -INFINITY) {
 #pragma unroll
-      for (int k = R - 1; k >= 0; --k)
+    for (int k = R - 1; k >= 0; --k)
 #pragma unroll
-        for (int e = 3; e >= 0; --e)
-          if (v[k][e] == mx) first = c0 + 4 * (tid + k * T) + e;
-    }
-    first = rules_block_min<T>(first, red);
+      for (int e = 3; e >= 0; --e)
+        if (v[k][e] >= near && rule_quotient(v[k][e], sc) == rule_quotient(mx, sc)) first = c0 + 4 * (tid + k * T) + e;
   }
   const unsigned long long hi = (unsigned long long)__float_as_uint(mx) << 32;
   unsigned long long* mine = wk.slots + (size_t)r * wk.pieces;
   if (!a.probs) {                                             // arg max alone: a second launch reads the words
+    first = rules_block_min<T>(first, red);
     if (tid == 0) {
       if (wk.pieces == 1) {
         const int id = mx > -INFINITY ? first : -1;
@@ -307,37 +325,39 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
 #pragma unroll
   for (int k = 0; k < R; ++k) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[k][e] = rule_exp(v[k][e] - safe);
+    for (int e = 0; e < 4; ++e) v[k][e] = rule_exp(v[k][e] - safe, sc);
     s += (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]);
   }
   s = rules_block_sum<T>(s, red);
   float f = s > 0.f ? 1.0f / s : 0.f;
-  if (wk.pieces == 1) {
-    if (a.argmax && tid == 0) {
-      const int id = mx > -INFINITY ? first : -1;
-      a.argmax[r] = id;
-      take_token(step.take, r, id);
-    }
-  } else {
+  int found = 1;                                              // 1: the row's token lies in this piece, 2: the piece is late, 0: neither
+  if (wk.pieces > 1) {
     if (tid < 64) {                                           // publish, then look for the row's words
       if (tid == 0) __hip_atomic_store(mine + piece, hi | __float_as_uint(s), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       RulesRow row;
       row.whole = false;
-      if (wk.looks >= 0) row = rules_collect(mine, wk.pieces, wk.looks);
+      if (wk.looks >= 0) row = rules_collect(mine, wk.pieces, wk.looks, sc);
       if (tid == 0) {
-        red[0] = !row.whole ? 1.f : mx > -INFINITY ? rule_exp(mx - row.mx) / row.sum : 0.f;
-        if (!row.whole) {
-          wk.late[(size_t)r * wk.pieces + piece] = 1u + (unsigned)first;
-          if (wk.looks >= 0) atomicAdd(wk.n_late, 1u);
-        } else if (a.argmax && row.winner == piece) {
-          const int id = row.mx > -INFINITY ? first : -1;
-          a.argmax[r] = id;
-          take_token(step.take, r, id);
-        }
+        red[0] = !row.whole ? 1.f : mx > -INFINITY ? rule_exp(mx - row.mx, sc) / row.sum : 0.f;
+        s_seq[0] = !row.whole ? 2 : row.winner == piece;
       }
     }
     __syncthreads();
     f = red[0];
+    found = s_seq[0];
+    __syncthreads();
+  }
+  if (found && (a.argmax || found == 2)) {
+    if (a.argmax) first = rules_block_min<T>(first, red);
+    if (tid == 0 && found == 1) {
+      const int id = mx > -INFINITY ? first : -1;
+      a.argmax[r] = id;
+      take_token(step.take, r, id);
+    }
+    if (tid == 0 && found == 2) {
+      wk.late[(size_t)r * wk.pieces + piece] = 1u + (unsigned)first;
+      if (wk.looks >= 0) atomicAdd(wk.n_late, 1u);
+    }
   }
 #pragma unroll
   for (int k = 0; k < R; ++k)
@@ -361,11 +381,17 @@ __global__ __launch_bounds__(256) void rules_late_kernel(ee_rules_call a, RulesS
     if (r < a.row_start[0] || r >= a.row_start[a.n_seq]) continue;      // (the whole workgroup; of no sequence: left as it is)
     const unsigned mark = wk.late[i];
     if (mark == 0) continue;
+    if (a.temperature) {
+      for (int b = threadIdx.x; b < a.n_seq; b += 256)
+        if (a.row_start[b] <= r && r < a.row_start[b + 1]) red[0] = a.temperature[b];
+    } else if (threadIdx.x == 0) red[0] = 1.f;
+    __syncthreads();
     if (threadIdx.x < 64) {
-      const RulesRow row = rules_collect(wk.slots + (size_t)r * wk.pieces, wk.pieces, 0);
+      const RuleScale sc = rule_scale(red[0]);
+      const RulesRow row = rules_collect(wk.slots + (size_t)r * wk.pieces, wk.pieces, 0, sc);
       if (threadIdx.x == 0) {
         const float mx = __uint_as_float((unsigned)(wk.slots[i] >> 32));
-        red[0] = mx > -INFINITY ? rule_exp(mx - row.mx) / row.sum : 0.f;
+        red[0] = mx > -INFINITY ? rule_exp(mx - row.mx, sc) / row.sum : 0.f;
         if (a.argmax && row.winner == piece) {
           const int id = row.mx > -INFINITY ? (int)(mark - 1u) : -1;
           a.argmax[r] = id;
@@ -412,16 +438,13 @@ __global__ __launch_bounds__(256) void rules_argmax_kernel(ee_rules_call a, Rule
 
 // ---- launch shapes ----
 static const int kRulesPieces[] = {1024, 2048, 4096, 8192};
-// The longest piece of which the launch still has two workgroups per compute unit (a longer piece reads the history and meets its row less often; beyond 8192 tokens,
-// by 512 threads, nothing is gained: 144 rows of 128256 tokens 53 us, in pieces of 16384 62, of 4096 55, of 2048 by 256 threads 82), or the shortest
-// that covers the vocabulary.
+// The longest piece of which the launch still has two workgroups per compute unit, up to 8192 tokens (a longer piece reads the history and meets its row less
+// often, but holds more of the table's LDS and of a compute unit's arithmetic: 144 rows of 128256 tokens 53 us, in pieces of 16384 62, of 4096 55, of 2048 82;
+// 96 whole rows of 32003 tokens 21 us, in pieces of 4096 19), or what covers the vocabulary.
 static int rules_piece(int rows, int vocab) {
   int piece = kRulesPieces[0];
-  for (int c : kRulesPieces) {
-    if (c != piece && (long)ceil_div(vocab, c) * rows < 512) break;
-    piece = c;
-    if (c >= vocab) break;
-  }
+  for (int c : kRulesPieces)
+    if (piece < vocab && (long)ceil_div(vocab, c) * rows >= 512) piece = c;
   return piece;
 }
 static size_t rules_words(int rows, int vocab) { return (size_t)rows * ceil_div(vocab, kRulesPieces[0]); }
