@@ -224,42 +224,61 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
   }
 }
 
-// A wave per (row, KV head): the partials of the row's items, in the plan's order.
+// A wave per (row, KV head).  Lane k fetches the statistics of the row's partial k and turns them into its weight; the partials themselves are then
+// fetched four loads at a time (a half or a quarter of the wave each, four dimensions a lane) with addresses and weights out of those lanes, so that nothing waits for
+// an index.  Sums in the plan's order.
 template <int D, bool ROWS>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedCall a) {
-  constexpr int LPR = D / 4;                           // lanes of a row (four dimensions each); the wave's halves (quarters) share out the partials
+  constexpr int LPR = D / 4, SUBS = 64 / LPR;          // lanes of a partial, partials fetched by one load of the wave
   const int lane = threadIdx.x & 63, w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = w % a.Hkv, j = w / a.Hkv;
   if (j >= a.n_joins) return;                          // whole wave
   const int4 jn = a.joins[j];                          // row, head, first entry, entries
   const int sub = lane / LPR, d = (lane % LPR) * 4;
-  constexpr int SUBS = 64 / LPR;
-  float mx = -INFINITY;
-  for (int k = lane; k < jn.w; k += 64) {
-    const int e = a.entries[jn.z + k];
-    mx = fmaxf(mx, a.part_ml[(((size_t)(e >> 4) * a.Hkv + kvh) * 16 + (e & 15)) * 2]);
-  }
-  for (int s = 1; s < 64; s <<= 1) mx = fmaxf(mx, __shfl_xor(mx, s, 64));
-  float den = 0.f;
+  float mx = -INFINITY, den = 0.f;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int k = sub; k < jn.w; k += SUBS) {
-    const int e = a.entries[jn.z + k];
-    const size_t at = ((size_t)(e >> 4) * a.Hkv + kvh) * 16 + (e & 15);
-    const float2 t = *(const float2*)(a.part_ml + at * 2);
-    const f32x4 x = *(const f32x4*)(a.part_o + at * D + d);
-    const float f = __builtin_amdgcn_exp2f(t.x - mx);
-    const bool some = t.y > 0.f;                       // (an item that this step did not reach has left no sum)
-    den += some ? f * t.y : 0.f;
+  for (int k0 = 0; k0 < jn.w; k0 += 64) {
+    const int n = min(64, jn.w - k0);
+    int e = 0;
+    float2 t = make_float2(-INFINITY, 0.f);
+    if (lane < n) {
+      e = a.entries[jn.z + k0 + lane];
+      e = ((e >> 4) * a.Hkv + kvh) * 16 + (e & 15);    // (row of part_o and part_ml)
+      t = *(const float2*)(a.part_ml + (size_t)e * 2);
+    }
+    float m = t.x;
+    for (int s = 1; s < n; s <<= 1) m = fmaxf(m, __shfl_xor(m, s, 64));      // (the first n lanes hold something)
+    m = fmaxf(__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m))), mx);
+    const float keep = __builtin_amdgcn_exp2f(mx - m);         // (of what the entries before left: 0 at first)
+    mx = m;
+    // (an item that this step did not reach has left no sum and no partial: weight 0, and its row is not read)
+    const float f = t.y > 0.f ? __builtin_amdgcn_exp2f(t.x - m) : 0.f;
+    float l = f * t.y;
+    for (int s = 1; s < n; s <<= 1) l += __shfl_xor(l, s, 64);
+    den = den * keep + __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(l)));
 #pragma unroll
-    for (int v = 0; v < 4; ++v) acc[v] += some ? f * x[v] : 0.f;
+    for (int v = 0; v < 4; ++v) acc[v] *= keep;
+    for (int q0 = 0; q0 < n; q0 += 4 * SUBS) {
+      f32x4 x[4];
+      float g[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = min(q0 + u * SUBS + sub, 63);
+        g[u] = __shfl(f, k, 64);
+        const int at = __shfl(e, k, 64);
+        x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (g[u] > 0.f) x[u] = *(const f32x4*)(a.part_o + (size_t)at * D + d);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[v] += g[u] * x[u][v];
+    }
   }
 #pragma unroll
-  for (int s = LPR; s < 64; s <<= 1) {
-    den += __shfl_xor(den, s, 64);
+  for (int s = LPR; s < 64; s <<= 1)
 #pragma unroll
     for (int v = 0; v < 4; ++v) acc[v] += __shfl_xor(acc[v], s, 64);
-  }
   if (sub == 0) {
     const float inv = 1.0f / den;
     store_out<D, ROWS>(a, jn.x, jn.y, kvh, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
