@@ -29,6 +29,10 @@ __device__ inline float colmax4(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Tables that nothing writes while a kernel runs, read through the scalar cache: a lookup by a vector load would count among the pages in flight,
+// and waiting for it would be waiting for them.
+typedef const __attribute__((address_space(4))) int* table_t;
+
 // Query and output of a row: the session's own layouts (q-tiles in fragment order, the O projection's operand), or row-major
 // (element (row, head, dim) at row * stride + head * D + dim).
 template <int D, bool ROWS>
@@ -44,7 +48,157 @@ __device__ inline void store_out(const SharedCall& a, int row, int head, int kvh
   *(uint2*)p = make_uint2(pack2(x, y), pack2(z, w));
 }
 
-// Workgroup = (KV head, item): up to eight packed q-tiles and a run of pages.  Four waves; wave w owns tiles w and w + 4.  A page reaches LDS by
+// where an item's tile leaves its results
+template <int D, bool ROWS>
+__device__ inline void store_tile(const SharedCall& a, int slot, int4 row, int kvh, int qc, int d, float inv, f32x4 x) {
+  if (slot < 0) {
+    if (row.x >= 0) store_out<D, ROWS>(a, row.x, row.y, kvh, d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  } else {
+    *(f32x4*)(a.part_o + (((size_t)slot * a.Hkv + kvh) * 16 + qc) * D + d) = x;
+  }
+}
+__device__ inline void store_stats(const SharedCall& a, int slot, int kvh, int qc, float m, float l) {
+  *(float2*)(a.part_ml + (((size_t)slot * a.Hkv + kvh) * 16 + qc) * 2) = make_float2(m, l);
+}
+
+// An item of one or two tiles: latency, not arithmetic, bounds it, so its pages go straight to registers, a page per wave: four waves (two of each tile) take
+// every fourth (second) page, 128 KiB in flight a workgroup, no barrier before the waves of a tile meet in LDS at the end.
+struct SharedItemView { int tile0, n_tiles, page0, npg, slot0, kv_end, first_masked; bool own; table_t bt; };
+template <int D, bool ROWS>
+__device__ __forceinline__ void shared_narrow(const SharedCall& a, const SharedItemView& it, int kvh, u32x4* lds) {
+  constexpr int DS = D / 32, DT = D / 16, KCH = 4 * DS;
+  const int lane = threadIdx.x & 63, g = lane >> 4, qc = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int parts = it.n_tiles == 1 ? 4 : 2, tile = it.n_tiles == 1 ? 0 : wave >> 1, w = it.n_tiles == 1 ? wave : wave & 1;
+  u32x4 kf[KCH], vf[KCH];
+  auto page_ptr = [&](int pg) __attribute__((always_inline)) {
+    return (const u32x4*)(a.kv + kv_slab(a.layer, it.bt[min(pg, it.npg - 1)], kvh, a.n_pages, a.Hkv, D)) + lane;
+  };
+  const u32x4* src = page_ptr(w);                                  // (a wave without a page reads the last one and drops it)
+#pragma unroll
+  for (int c = 0; c < KCH; ++c) kf[c] = src[c * 64];
+#pragma unroll
+  for (int c = 0; c < KCH; ++c) vf[c] = src[(KCH + c) * 64];
+  const int4 row = a.rows[(it.tile0 + tile) * 16 + qc];
+  const int limit = row.x < 0 ? -1 : it.own ? row.w + a.pos_add : INT_MAX;
+  const bf16_t* q = q_address<D, ROWS>(a, row, kvh, g);
+  u32x4 qf[DS];
+#pragma unroll
+  for (int s = 0; s < DS; ++s) qf[s] = *(const u32x4*)(q + s * (ROWS ? 32 : 512));
+  const float sc2 = 1.4426950408889634f / sqrtf((float)D);         // scores in base-2 units
+  const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+  float mrun = -INFINITY;
+  f32x4 o[DT], lacc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto step = [&](auto more, int pg) __attribute__((always_inline)) {
+    const int base = (it.page0 + pg) * EE_PAGE + 16 * g;           // this lane group holds positions base .. base+15
+    const u32x4* next = decltype(more)::value ? page_ptr(pg + parts) : nullptr;
+    f32x4 s4[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s4[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < DS; ++s)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s4[t] = mfma16(kf[t * DS + s], qf[s], s4[t]);
+    __builtin_amdgcn_sched_barrier(0);                             // (no request before its registers are free)
+    if (decltype(more)::value) {                                   // (the next page's fragments are requested as soon as this page's are consumed)
+#pragma unroll
+      for (int c = 0; c < KCH; ++c) kf[c] = next[c * 64];
+    }
+    const bool masked = pg >= it.first_masked;                     // (uniform)
+    const int seen = limit - base, live = it.kv_end - base;        // of this lane group's positions: the last seen, the first dead
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        if (4 * t + v > seen) s4[t][v] = -INFINITY;
+        tmax = fmaxf(tmax, s4[t][v]);
+      }
+    tmax = colmax4(tmax * sc2);
+    const float mnew = fmaxf(mrun, tmax);
+    const float msafe = mnew == -INFINITY ? 0.f : mnew;
+    const float alpha = __builtin_amdgcn_exp2f(mrun - msafe), nm = -msafe;
+    mrun = mnew;
+    uint32_t pk[8];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      pk[2 * t] = pack2(__builtin_amdgcn_exp2f(fmaf(s4[t][0], sc2, nm)), __builtin_amdgcn_exp2f(fmaf(s4[t][1], sc2, nm)));
+      pk[2 * t + 1] = pack2(__builtin_amdgcn_exp2f(fmaf(s4[t][2], sc2, nm)), __builtin_amdgcn_exp2f(fmaf(s4[t][3], sc2, nm)));
+    }
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) { o[dt][0] *= alpha; o[dt][1] *= alpha; o[dt][2] *= alpha; o[dt][3] *= alpha; }
+      lacc[0] *= alpha; lacc[1] *= alpha; lacc[2] *= alpha; lacc[3] *= alpha;
+    }
+    const u32x4 P[2] = {u32x4{pk[0], pk[1], pk[2], pk[3]}, u32x4{pk[4], pk[5], pk[6], pk[7]}};
+    if (masked) {      // dead positions (>= kv_end) may hold anything: zero their V
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t keep = 8 * ks + 2 * j + 1 < live ? 0xffffffffu : (8 * ks + 2 * j < live ? 0xffffu : 0u);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) vf[dt * 2 + ks][j] &= keep;
+        }
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      lacc = mfma16(ones, P[ks], lacc);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma16(vf[dt * 2 + ks], P[ks], o[dt]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (decltype(more)::value) {
+#pragma unroll
+      for (int c = 0; c < KCH; ++c) vf[c] = next[(KCH + c) * 64];
+    }
+  };
+  if (w < it.npg) {
+    int pg = w;
+    for (; pg + parts < it.npg; pg += parts) step(std::true_type{}, pg);
+    step(std::false_type{}, pg);
+  }
+  f32x4* lo = (f32x4*)lds;                                         // [wave][d-tile][lane]
+  float2* ml = (float2*)(lds + 4 * DT * 64);                       // [wave][lane]
+  ml[wave * 64 + lane] = make_float2(mrun, lacc[0]);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) lo[(wave * DT + dt) * 64 + lane] = o[dt];
+  __syncthreads();
+  // the waves of a tile share out its d-tiles, each over the parts in order
+  const int w0 = wave - w;
+  float mall = -INFINITY, l = 0.f, f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < parts) mall = fmaxf(mall, ml[(w0 + i) * 64 + lane].x);
+  const float msafe = mall == -INFINITY ? 0.f : mall;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[i] = 0.f;
+    if (i < parts) {
+      const float2 t = ml[(w0 + i) * 64 + lane];
+      f[i] = __builtin_amdgcn_exp2f(t.x - msafe);
+      l += f[i] * t.y;
+    }
+  }
+  const int slot = it.slot0 < 0 ? -1 : it.slot0 + tile;
+  const float inv = 1.0f / l;
+  if (slot >= 0 && w == 0 && g == 0) store_stats(a, slot, kvh, qc, mall, l);
+  const int share = DT / parts;
+  for (int dt = w * share; dt < (w + 1) * share; ++dt) {
+    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < parts) {
+        const f32x4 y = lo[((w0 + i) * DT + dt) * 64 + lane];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[v] += f[i] * y[v];
+      }
+    store_tile<D, ROWS>(a, slot, row, kvh, qc, dt * 16 + 4 * g, inv, x);
+  }
+}
+
+// Workgroup = (KV head, item): up to eight packed q-tiles and a run of pages.  Items of more than two tiles: wave w owns tiles w and w + 4.  A page reaches LDS by
 // direct global->LDS loads, two slots, one barrier a page; two workgroups share a compute unit, so that one's softmax, start and end run under the
 // other's matrix instructions and loads.
 template <int D, bool ROWS>
@@ -55,10 +209,10 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
   const int lane = threadIdx.x & 63, g = lane >> 4, qc = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x;
-  const int* it = a.items + 8 * blockIdx.y;
+  const table_t it = (table_t)(uintptr_t)a.items + 8 * blockIdx.y, seq_p0 = (table_t)(uintptr_t)a.seq_p0, seq_m = (table_t)(uintptr_t)a.seq_m;
   const int tile0 = it[0], n_tiles = it[1], seq = it[2], page0 = it[3], slot0 = it[5];
   const bool own = it[6] != 0;
-  const int kv_end = own ? a.seq_p0[seq] + a.seq_m[seq] + a.pos_add : INT_MAX;
+  const int kv_end = own ? seq_p0[seq] + seq_m[seq] + a.pos_add : INT_MAX;
   const int page1 = own ? min(it[4], (kv_end + EE_PAGE - 1) / EE_PAGE) : it[4];
   if (page0 >= page1) {                                // a run that this step does not reach yet: nothing to join (whole workgroup)
     if (slot0 >= 0 && threadIdx.x < n_tiles * 16)
@@ -66,7 +220,13 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
     return;
   }
   const int npg = page1 - page0;
-  const int* bt = a.block_table + (size_t)seq * a.pps + page0;
+  const table_t bt = (table_t)(uintptr_t)a.block_table + (size_t)seq * a.pps + page0;
+  // pages before this one are seen whole by every row of the item
+  const int first_masked = own ? (((table_t)(uintptr_t)a.rows)[tile0 * 64 + 3] + a.pos_add + 1) / EE_PAGE - page0 : npg;
+  if (n_tiles <= 2) {
+    shared_narrow<D, ROWS>(a, SharedItemView{tile0, n_tiles, page0, npg, slot0, kv_end, first_masked, own, bt}, kvh, &lds[0][0]);
+    return;
+  }
   typedef const __attribute__((address_space(1))) void* gptr_t;
   typedef __attribute__((address_space(3))) void* lptr_t;
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lptr_t)&lds[0][0]);
@@ -78,8 +238,6 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
   };
   request(0, bt[0]);
   int next_page = bt[min(1, npg - 1)];
-  // pages before this one are seen whole by every row of the item
-  const int first_masked = own ? (a.rows[tile0 * 16].w + a.pos_add + 1) / EE_PAGE - page0 : npg;
   const int nt = (wave < n_tiles) + (wave + 4 < n_tiles);          // tiles of this wave
   int limit[2];
   int4 row[2];
@@ -132,7 +290,7 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          if (MASKED && base + 4 * t + v > limit[i]) s4[i][t][v] = -INFINITY;
+          if (MASKED && 4 * t + v > limit[i] - base) s4[i][t][v] = -INFINITY;
           tmax = fmaxf(tmax, s4[i][t][v]);
         }
       tmax = colmax4(tmax * sc2);
@@ -171,8 +329,7 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
           if (MASKED) {     // dead positions (>= kv_end) may hold anything: zero their V
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int pa = base + 8 * ks + 2 * j;
-              v[j] &= pa + 1 < kv_end ? 0xffffffffu : (pa < kv_end ? 0xffffu : 0u);
+              v[j] &= 8 * ks + 2 * j + 1 < kv_end - base ? 0xffffffffu : (8 * ks + 2 * j < kv_end - base ? 0xffffu : 0u);
             }
           }
 #pragma unroll
@@ -207,20 +364,11 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedCall a) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (i >= nt) break;
-    const float l = lacc[i][0];
-    if (slot0 < 0) {
-      if (row[i].x < 0) continue;
-      const float inv = 1.0f / l;
+    const int slot = slot0 < 0 ? -1 : slot0 + wave + 4 * i;
+    if (slot >= 0 && g == 0) store_stats(a, slot, kvh, qc, mrun[i], lacc[i][0]);
+    const float inv = 1.0f / lacc[i][0];
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        store_out<D, ROWS>(a, row[i].x, row[i].y, kvh, dt * 16 + 4 * g, o[i][dt][0] * inv, o[i][dt][1] * inv, o[i][dt][2] * inv, o[i][dt][3] * inv);
-    } else {
-      const size_t at = ((size_t)(slot0 + wave + 4 * i) * a.Hkv + kvh) * 16 + qc;
-      if (g == 0) *(float2*)(a.part_ml + at * 2) = make_float2(mrun[i], l);
-      float* p = a.part_o + at * D + 4 * g;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) *(f32x4*)(p + dt * 16) = o[i][dt];
-    }
+    for (int dt = 0; dt < DT; ++dt) store_tile<D, ROWS>(a, slot, row[i], kvh, qc, dt * 16 + 4 * g, inv, o[i][dt]);
   }
 }
 
