@@ -81,8 +81,16 @@ inline void shared_segments(const std::vector<SharedSeq>& q, const std::vector<i
   }
 }
 
-// Cost of an item in microseconds on its half of a compute unit, by measurement (shared_attn_kernel).
-inline double shared_item_us(int tiles, int pages) { return 4.5 + pages * (0.8 + 0.25 * tiles); }
+// Cost of an item in microseconds on its half of a compute unit: fitted to 484 timings (eleven batches of 2 to 64 sequences, each cut in 44 ways;
+// the cuts that the fit chooses take 1.03 of the quickest ones' time in the mean, 1.09 at the worst).  Of one or two tiles, four or two pages
+// go at a time; of more, every page costs its way through LDS and its tiles' products, 1.13 times that where
+// the other half of every unit has such an item too (both: 0 with no unit shared so, 1 with all).
+inline double shared_item_us(int tiles, int pages, double both) {
+  if (tiles <= 2) return 1.7 * (tiles == 1 ? (pages + 3) / 4 : (pages + 1) / 2);
+  return pages * (0.77 + 0.125 * tiles) * (1 + 0.13 * both);
+}
+constexpr double kSharedSlotUs = 0.034;               // a tile's partial results written, read and joined
+constexpr double kSharedPageUs = 2.7;                 // a page of every KV head read from memory: this by the places that run at a time
 
 // rep: query heads per KV head; most_slots: room for partial results; wgs: items of one KV head that run at a time; least: pages of
 // a shared segment at the least; share: false keeps every sequence to itself; per_forced > 0: pages per item.
@@ -119,8 +127,13 @@ inline SharedPlan plan_shared(const std::vector<SharedSeq>& q, int rep, int most
   int longest[2] = {1, 1};                              // shared, own
   for (const SharedSegment& s : segs) longest[s.own] = std::max(longest[s.own], s.page1 - s.page0);
   std::vector<double> free_at;
+  long distinct = 0;
+  for (const SharedSegment& s : segs) distinct += s.page1 - s.page0;
   auto schedule = [&](const int* per, double& us) {
-    long slots = 0;
+    long slots = 0, wide = 0;
+    for (size_t i = 0; i < segs.size(); ++i)
+      wide += (long)shared_cuts(segs[i].page1 - segs[i].page0, per[segs[i].own]).cuts * ((at[i].tiles + block / 2 - 1) / block);
+    const double both = std::min(1.0, std::max(0.0, 2.0 * wide / wgs - 1));
     free_at.assign(wgs, 0.0);
     double end = 0;
     for (int own = 0; own < 2; ++own)
@@ -133,12 +146,12 @@ inline SharedPlan plan_shared(const std::vector<SharedSeq>& q, int rep, int most
           for (int t = 0; t < at[i].tiles; t += block) {
             std::pop_heap(free_at.begin(), free_at.end(), std::greater<double>());
             double& f = free_at.back();
-            f += shared_item_us(std::min(block, at[i].tiles - t), std::min(run, n - c * run));
+            f += shared_item_us(std::min(block, at[i].tiles - t), std::min(run, n - c * run), both);
             end = std::max(end, f);
             std::push_heap(free_at.begin(), free_at.end(), std::greater<double>());
           }
       }
-    us = end + 0.012 * slots;
+    us = std::max(end, kSharedPageUs * distinct / wgs) + kSharedSlotUs * slots;
     return slots <= most_slots;
   };
   int per[2] = {longest[0], longest[1]};
@@ -160,11 +173,6 @@ inline SharedPlan plan_shared(const std::vector<SharedSeq>& q, int rep, int most
         if (schedule(p, us) && us < best) { best = us; per[0] = joint; per[1] = own; }
       }
   }
-#ifdef SP_PROBE
-  if (getenv("SP_S")) per[0] = std::max(1, (longest[0] + atoi(getenv("SP_S")) - 1) / atoi(getenv("SP_S")));
-  if (getenv("SP_O")) per[1] = std::max(1, (longest[1] + atoi(getenv("SP_O")) - 1) / atoi(getenv("SP_O")));
-  { double us = 0; schedule(per, us); static int said = 0; if (said++ < 1 || getenv("SP_SAY")) fprintf(stderr, "plan: per %d %d of %d %d, items of %zu segments, model %.1f us\n", per[0], per[1], longest[0], longest[1], segs.size(), us); }
-#endif
   // items: the cuts of a segment one after the other, all its blocks of a cut together, so that workgroups that run at the same time read the same pages
   std::vector<int> slot_of;                             // per segment: first slot
   std::vector<int> cuts_of(segs.size());
