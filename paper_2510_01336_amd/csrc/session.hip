@@ -461,24 +461,30 @@ static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool a
   }
   std::vector<SharedSeq> q(s->B);
   const int* h = s->slot[si].h;
+  long named = 0;
   for (int b = 0; b < s->B; ++b) {
     if (!p.m[b]) continue;
     q[b].m = p.m[b]; q[b].p0 = p.p0[b]; q[b].row0 = h[s->o_seq_row0 + b]; q[b].qt0 = h[s->o_seq_qt0 + b];
     q[b].n_pages = ceil_div(p.p0[b] + p.m[b] + steps - 1, EE_PAGE);
     q[b].pages = s->seq[b].pages.data();
+    named += q[b].n_pages;
   }
   const int wgs = std::max(1, 512 / s->m->cfg.n_kv_heads);      // (two workgroups a compute unit)
-  SharedPlan P = plan_shared(q, rep, (int)s->part_units, wgs, 2, true);
+  if (!always && g_shared_attention < 0 && !shared_pays(named, wgs, 0)) return EE_OK;
+  // A run of one page is not worth a segment: 16 to 48 sequences behind 4096 shared positions, in groups that share one page more, take 0.1 to
+  // 0.6 us longer with it than without; of 2 and 4 pages it is the same either way, of 8 the segment saves up to 6 us.
+  const int least = 2;
+  SharedPlan P = plan_shared(q, rep, (int)s->part_units, wgs, least, true);
   SharedSlot& sl = s->shared[si];
   auto fits = [&](const SharedPlan& x) {
     return 8 * x.items.size() + 4 * x.rows.size() + 4 * x.joins.size() + x.entries.size() + 16 <= s->shared_cap && (size_t)x.slots <= s->part_units;
   };
-  if (!fits(P) && always) P = plan_shared(q, rep, (int)s->part_units, wgs, 2, false);      // (every sequence by itself, uncut if need be)
+  if (!fits(P) && always) P = plan_shared(q, rep, (int)s->part_units, wgs, least, false);      // (every sequence by itself, uncut if need be)
   if (!fits(P)) {
     if (always) { ee_set_error("internal: the tables of %d rows do not fit", p.M); return EE_ERR_CAPACITY; }
     return EE_OK;
   }
-  if (!always && (!P.shares || (g_shared_attention < 0 && !shared_pays(P)))) return EE_OK;
+  if (!always && (!P.shares || (g_shared_attention < 0 && !shared_pays(P.pages_named, wgs, P.us)))) return EE_OK;
   if (sl.in_flight) { HIP_TRY(hipEventSynchronize(sl.copied)); sl.in_flight = false; }
   size_t o = 0;
   auto put = [&](const void* src, size_t n) {
