@@ -325,15 +325,21 @@ static void drop_page(ee_session* s, int pg) {
   if (--s->page_ref[pg] == 0) s->free_pages.push_back(pg);
 }
 // pages that a call has to take for its sequences to hold positions [0, want_positions[b]) (0: not taking part), pages of their own
-// from the pending token's position on
+// from the pending token's position on (of a page that all of its sequences write, the last one keeps it)
 static int pages_needed_total(const ee_session* s, const std::vector<int>& want_positions) {
   int need = 0;
+  std::vector<int> copies;
   for (int b = 0; b < s->B; ++b) {
     const SeqState& q = s->seq[b];
     int have = (int)q.pages.size(), want = ceil_div(want_positions[b], EE_PAGE);
     if (want > have) need += want - have;
-    if (want_positions[b] > 0)
-      for (int i = std::max(0, (int)(q.C.size() + q.V.size()) - 1) / EE_PAGE; i < have; ++i) need += s->page_ref[q.pages[i]] > 1;
+    if (want_positions[b] <= 0) continue;
+    for (int i = std::max(0, (int)(q.C.size() + q.V.size()) - 1) / EE_PAGE; i < have; ++i) {
+      const int pg = q.pages[i];
+      if (s->page_ref[pg] < 2) continue;
+      copies.resize(s->n_pages, 0);
+      if (++copies[pg] < s->page_ref[pg]) ++need;
+    }
   }
   return need;
 }
@@ -477,7 +483,7 @@ static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool a
   SharedPlan P = plan_shared(q, rep, (int)s->part_units, wgs, least, true);
   SharedSlot& sl = s->shared[si];
   auto fits = [&](const SharedPlan& x) {
-    return 8 * x.items.size() + 4 * x.rows.size() + 4 * x.joins.size() + x.entries.size() + 16 <= s->shared_cap && (size_t)x.slots <= s->part_units;
+    return x.items.size() < 65536 && 8 * x.items.size() + 4 * x.rows.size() + 4 * x.joins.size() + x.entries.size() + 16 <= s->shared_cap && (size_t)x.slots <= s->part_units;
   };
   if (!fits(P) && always) P = plan_shared(q, rep, (int)s->part_units, wgs, least, false);      // (every sequence by itself, uncut if need be)
   if (!fits(P)) {

@@ -249,3 +249,25 @@ def test_capacity_of_a_copy():
         sess.prefill_shared([-1, 0], [None, p[:66]])             # one shared page and one too many
     assert e.value.code == -3
     sess.close(); model.close()
+
+
+def test_two_copies_of_one_page():
+    """Two sequences rolled back into the page that they share: the first gets a copy, the other keeps the page, and one free page is enough."""
+    cfg = bf16_small()
+    p, other = synth.gen_prompt(cfg.vocab, 190, 1), synth.gen_prompt(cfg.vocab, 80, 2)
+    model = hs.Model(cfg, 10)
+    roomy, tight = hs.Session(model, 3, 200, 10), hs.Session(model, 3, 200, 10, 4)
+    toks = []
+    for sess in (roomy, tight):
+        sess.prefill_seq(0, p[:120])
+        sess.prefill_shared([-1, 0, -1], [None, p[:100], None])
+        sess.rollback(0, 0b111, 30)
+        sess.rollback(1, 0b111, 20)
+        sess.prefill_seq(2, other)
+        assert sess.shared_pages(0) == sess.shared_pages(1) == 1
+        if sess is tight:
+            assert sess.free_pages() == 1
+        toks.append(sess.decode_ar(4))
+        assert sess.shared_pages(0) == sess.shared_pages(1) == 0
+    assert tight.free_pages() == 0 and np.array_equal(*toks)
+    roomy.close(); tight.close(); model.close()
