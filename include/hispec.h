@@ -121,7 +121,8 @@ void ee_model_free(ee_model* m);   /* frees host bookkeeping only; the arena is 
  *   total_pages : size of the shared page pool, 0 = batch * ceil(max_ctx/64)
  * ee_session_bytes() counts the work buffers of context-build passes of up to 4096 rows (EE_BF16; no more than the
  * sequences or the page pool can hold).  ee_session_create() also takes a smaller arena and then makes the passes
- * shorter, in steps of 512 rows down to 512 (EE_ERR_CAPACITY below that).  A row of a pass costs about 70 KB at
+ * shorter, in steps of 512 rows down to 512; the tables of attention over shared pages go last (ee_attend_begin then
+ * refuses, the other calls read every sequence's pages by themselves); EE_ERR_CAPACITY below that.  A row of a pass costs about 70 KB at
  * d_model 4096 / d_ffn 14336 and 140 KB at 8192 / 28672: passes of 512 rows need 0.25 and 0.5 GB less than passes of
  * 4096; a long context build then takes up to half as long again.          */
 size_t ee_session_bytes(const ee_model* m, int batch, int max_ctx, int max_rows, int total_pages);
@@ -294,7 +295,7 @@ int ee_debug_read_dist(ee_session* s, int which, int seq, int row0, int n, float
  * overlap q.  Nothing is synchronised: the calls can be captured into a graph and replayed while ee_attend_begin
  * stays valid (work buffers are the session's: graphs and calls of one session may not overlap in time).
  * EE_ERR_ARG: bad rows, positions or layer, or the layer's group does not hold the positions; EE_ERR_STATE: no valid begin,
- * or a sequence without a context. */
+ * or a sequence without a context; EE_ERR_CAPACITY: the session's arena is too small for the tables. */
 int ee_attend_begin(ee_session* s, const int32_t* rows, const int32_t* pos0);
 int ee_attend(ee_session* s, int layer, const void* q, int dtype, int64_t q_stride, void* out, int64_t out_stride);
 

@@ -107,6 +107,7 @@ struct ee_session {
   float *Z = nullptr, *T = nullptr, *ssq_t = nullptr, *ones = nullptr;
   void* TF = nullptr;
   SharedSlot shared[2];
+  bool shared_room = true;      // the arena has room for them
   size_t shared_cap = 0;        // ints of one of them
   bool attend_ready = false;    // ee_attend_begin's metadata (slot 0) and tables are in place
   std::vector<int> attend_end;  // positions that its rows see, per sequence (0: takes no part)
@@ -212,7 +213,8 @@ static size_t carve(ee_session* s, char* base) {
     s->gemm_part = s->maxM > 64 ? cv.take<float>(gp) : nullptr;
     s->inv_rms = cv.take<float>(s->inv_cap);
   }
-  if (bf) {      // rows of at most four segments each, items and entries of as many partials as there is room for
+  s->shared_cap = 0;
+  if (bf && s->shared_room) {      // rows of at most four segments each, items and entries of as many partials as there is room for
     const size_t packed = 4 * (size_t)s->headM * rep + 16 * (size_t)s->B, joins = (size_t)s->headM * rep;
     s->shared_cap = 4 * packed + 8 * (packed / 16 + s->part_units) + 4 * joins + 16 * s->part_units;
     for (SharedSlot& sl : s->shared) sl.d = cv.take<int>(s->shared_cap);
@@ -270,6 +272,10 @@ extern "C" int ee_session_create(ee_model* m, int batch, int max_ctx, int max_ro
   for (int most = kMostPassRows; (s->bytes = carve(s, s->base)) > arena_bytes && most > kLeastPassRows;) {
     most = std::max(kLeastPassRows, s->chunk - 512);
     shape_session(s, m, batch, max_ctx, max_rows, total_pages, most);
+  }
+  if (s->bytes > arena_bytes && s->shared_cap) {       // ... and at the last no tables of attention over shared pages
+    s->shared_room = false;
+    s->bytes = carve(s, s->base);
   }
   if (arena_bytes < s->bytes) {
     ee_set_error("session arena too small: %zu < %zu", arena_bytes, s->bytes);
@@ -457,7 +463,7 @@ extern int g_shared_attention;
 int g_shared_attention = -1;         // test hook: 1 wherever pages are shared, 0 never, -1 the built-in choice
 static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool always = false) {
   p.shared = nullptr;
-  if (!s->m->bf16) return EE_OK;
+  if (!s->m->bf16 || (!always && !s->shared_room)) return EE_OK;
   const int rep = s->m->cfg.n_q_heads / s->m->cfg.n_kv_heads;
   if (!always) {
     if (g_shared_attention == 0 || g_attn_form >= 0 || g_attn_pages_override > 0) return EE_OK;
@@ -1732,6 +1738,7 @@ extern "C" int ee_attend_begin(ee_session* s, const int32_t* rows, const int32_t
     any++;
   }
   if (!any) { ee_set_error("no query rows are given"); return EE_ERR_ARG; }
+  if (s->m->bf16 && !s->shared_room) { ee_set_error("the session's arena has no room for the tables of this call (ee_session_bytes)"); return EE_ERR_CAPACITY; }
   EE_TRY(build_meta(s, 0, p, [](int, int, int&, int&, int&) {}, 0, false));
   EE_TRY(upload_meta(s, 0));
   EE_TRY(share_attention(s, 0, p, 1, true));

@@ -397,3 +397,59 @@ def test_samples_of_one_prompt_under_rules():
         sess.release(b)
     assert sess.free_pages() == total
     sess.close(); model.close()
+
+
+def test_built_in_choice():
+    """Where many sequences share much a call takes the shared form by itself, where little is shared it does not; both agree."""
+    cfg = config(32, 8, 128)
+    model = hs.Model(cfg, 1)
+    for B, prefix, taken in ((48, 2600, True), (3, 300, False)):
+        prompts = prompts_of(cfg.vocab, prefix, [20 + b for b in range(B)])
+        sess = hs.Session(model, B, prefix + 100, 4)
+        sess.enable_logits(True)
+        sess.prefill_seq(0, prompts[0])
+        sess.prefill_shared([-1] + [0] * (B - 1), [None] + prompts[1:])
+        lens = sess.lengths()[:, 0]
+        logits = []
+        for mode in (-1, 0):
+            hs.ee_debug_shared_attention(mode)
+            sess.decode_ar(1)
+            assert (hs.ee_debug_last_attention(sess.handle) == 3) == (taken and mode == -1), (B, mode)
+            logits.append(sess.last_logits().copy())
+            for b in range(B):
+                sess.rollback(b, 0b111, int(lens[b]))
+        assert max_rel(*logits) <= 2e-2
+        sess.close()
+    model.close()
+
+
+def test_arena_without_room_for_the_tables():
+    """In the smallest arena a session shares pages and decodes as ever, by sequences; attention of given rows is refused."""
+    cfg = bf16_d128()
+    model = hs.Model(cfg, 4)
+    prompts = prompts_of(cfg.vocab, 700, [30, 5])
+    hs.ee_debug_shared_attention(1)
+    full = hs.ee_session_bytes(model.handle, 2, 2000, 8, 0)
+    with pytest.raises(hs.EEError) as e:
+        hs.Session(model, 2, 2000, 8, arena_bytes=4096)
+    least = int(str(e.value).split("<")[1])                      # (of passes of 512 rows, without the tables)
+    assert least < full
+    toks = []
+    for size, form in ((full, True), (least, False)):
+        sess = hs.Session(model, 2, 2000, 8, arena_bytes=size)
+        sess.enable_logits(True)
+        sess.prefill_seq(0, prompts[0])
+        sess.prefill_shared([-1, 0], [None, prompts[1]])
+        assert sess.shared_pages(1) == 10
+        if form:
+            sess.attend_begin([1, 1])
+        else:
+            with pytest.raises(hs.EEError) as e:
+                sess.attend_begin([1, 1])
+            assert e.value.code == -3
+        sess.decode_ar(1)
+        assert (hs.ee_debug_last_attention(sess.handle) == 3) == form
+        toks.append(sess.last_logits().copy())
+        sess.close()
+    assert max_rel(*toks) <= 2e-2
+    model.close()
