@@ -482,7 +482,7 @@ static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool a
     named += q[b].n_pages;
   }
   const int wgs = std::max(1, 512 / s->m->cfg.n_kv_heads);      // (two workgroups a compute unit)
-  if (!always && g_shared_attention < 0 && !shared_pays(named, wgs, 0)) return EE_OK;
+  if (!always && g_shared_attention < 0 && !shared_pays(named, wgs, kSharedJoinUs)) return EE_OK;
   // A run of one page is not worth a segment: 16 to 48 sequences behind 4096 shared positions, in groups that share one page more, take 0.1 to
   // 0.6 us longer with it than without; of 2 and 4 pages it is the same either way, of 8 the segment saves up to 6 us.
   const int least = 2;
@@ -491,6 +491,10 @@ static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool a
   auto fits = [&](const SharedPlan& x) {
     return x.items.size() < 65536 && 8 * x.items.size() + 4 * x.rows.size() + 4 * x.joins.size() + x.entries.size() + 16 <= s->shared_cap && (size_t)x.slots <= s->part_units;
   };
+  if (always && P.shares && named <= 4 * wgs) {          // few pages: uncut and unshared a call needs no joining, one launch instead of two
+    SharedPlan one = plan_shared(q, rep, (int)s->part_units, wgs, least, false);
+    if (fits(one) && one.us < P.us) P = std::move(one);
+  }
   if (!fits(P) && always) P = plan_shared(q, rep, (int)s->part_units, wgs, least, false);      // (every sequence by itself, uncut if need be)
   if (!fits(P)) {
     if (always) { ee_set_error("internal: the tables of %d rows do not fit", p.M); return EE_ERR_CAPACITY; }

@@ -89,6 +89,7 @@ inline double shared_item_us(int tiles, int pages, double both) {
   return pages * (0.77 + 0.125 * tiles) * (1 + 0.13 * both);
 }
 constexpr double kSharedSlotUs = 0.034;               // a tile's partial results written, read and joined
+constexpr double kSharedJoinUs = 3.5;                 // the launch that joins them
 constexpr double kSharedPageUs = 2.7;                 // a page of every KV head read from memory: this by the places that run at a time
 
 // rep: query heads per KV head; most_slots: room for partial results; wgs: items of one KV head that run at a time; least: pages of
@@ -129,27 +130,28 @@ inline SharedPlan plan_shared(const std::vector<SharedSeq>& q, int rep, int most
   // are done soonest, the joining of the partial results counted in.  Segments alike are dealt together, and a pair is only dealt if the
   // work over all places and the longest item leave it a chance: the whole choice takes some microseconds of the host.
   int longest[2] = {1, 1};                              // shared, own
-  struct Alike { int tiles, pages, own, n; };
+  struct Alike { int tiles, pages, own, alone, n; };      // alone: its rows have no other segment, so that uncut they need no joining
   std::vector<Alike> alike;
   long distinct = 0;
   for (size_t i = 0; i < segs.size(); ++i) {
     const int n = segs[i].page1 - segs[i].page0;
     longest[segs[i].own] = std::max(longest[segs[i].own], n);
     distinct += n;
-    if (!alike.empty() && alike.back().tiles == at[i].tiles && alike.back().pages == n && alike.back().own == (int)segs[i].own) alike.back().n++;
-    else alike.push_back({at[i].tiles, n, (int)segs[i].own, 1});
+    const Alike x = {at[i].tiles, n, segs[i].own, segs[i].page0 == 0 && segs[i].own, 1};
+    if (!alike.empty() && alike.back().tiles == x.tiles && alike.back().pages == n && alike.back().own == x.own && alike.back().alone == x.alone) alike.back().n++;
+    else alike.push_back(x);
   }
   std::vector<double> free_at;
   auto schedule = [&](const int* per, double best, double& us) {
     long slots = 0, wide = 0, items = 0;
     for (const Alike& s : alike) {
       const int cuts = shared_cuts(s.pages, per[s.own]).cuts;
-      slots += (long)s.n * s.tiles * cuts;
+      if (cuts > 1 || !s.alone) slots += (long)s.n * s.tiles * cuts;
       items += (long)s.n * cuts * ((s.tiles + block - 1) / block);
       wide += (long)s.n * cuts * ((s.tiles + block / 2 - 1) / block);
     }
     if (slots > most_slots) return false;
-    const double both = std::min(1.0, std::max(0.0, 2.0 * wide / wgs - 1)), more = kSharedSlotUs * slots;
+    const double both = std::min(1.0, std::max(0.0, 2.0 * wide / wgs - 1)), more = kSharedSlotUs * slots + (slots ? kSharedJoinUs : 0);
     auto each = [&](auto deal) {                        // runs of equal items, in their order
       for (const Alike& s : alike) {
         const auto [cuts, run] = shared_cuts(s.pages, per[s.own]);
@@ -239,9 +241,9 @@ inline SharedPlan plan_shared(const std::vector<SharedSeq>& q, int rep, int most
 
 // Whether a call of a session takes the plan instead of reading every sequence's pages by itself, which takes the time of the pages that the
 // sequences name, a page of every KV head 1.8 us by the places that run at a time (from the caches, 9.3 TB/s; shared ones lie there).  The
-// plan's launches and waits cost 6 us more than theirs.  Measured on calls of 14 layers, 8 KV heads, 114 batches of 2 to 48 sequences
+// plan's launches and waits cost 6 us more than theirs, the launch that joins among them.  Measured on calls of 14 layers, 8 KV heads, 114 batches of 2 to 48 sequences
 // that share 128 to 8192 positions, 20 to 1500 of their own, 1 and 8 rows each, both forms: the rule takes the slower form of seven, 0.1 to 2.3 us a
 // layer slower.  A whole call of 48 sequences that share 8192 positions takes 3220 us by sequences and 1220 by the plan (eight rows each:
 // 4195 and 2703), of 16 that share 2048 630 and 662 (the largest loss), of 4 that share 256 616 and 703 with eight rows (left to the
 // other form).  A plan for every batch that names twice the pages that it reads lost 150 us a layer over the 114.
-inline bool shared_pays(long pages_named, int wgs, double plan_us) { return plan_us + 6.0 < 1.8 * pages_named / wgs; }
+inline bool shared_pays(long pages_named, int wgs, double plan_us) { return plan_us + 2.5 < 1.8 * pages_named / wgs; }
