@@ -276,6 +276,8 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
     }
     own = fmaxf(own, fmaxf(fmaxf(v[k][0], v[k][1]), fmaxf(v[k][2], v[k][3])));
   }
+  // (non-temporal: rows that are written once would push rows that are being read out of the caches; 512 softmaxes of 128256 tokens 143 -> 128 us,
+  // 144 rows 51 -> 49, while non-temporal loads lose 2 us of 49)
   auto store = [&]() {
     float* y = a.out + out0;
 #pragma unroll
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(T) void rules_kernel(ee_rules_call a, RulesStep ste
       if (i + 3 < cn) {
         f32x4u f;
         f[0] = v[k][0]; f[1] = v[k][1]; f[2] = v[k][2]; f[3] = v[k][3];
-        *(f32x4u*)(y + i) = f;
+        __builtin_nontemporal_store(f, (f32x4u*)(y + i));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) if (i + e < cn) y[i + e] = v[k][e];
@@ -438,9 +440,9 @@ __global__ __launch_bounds__(256) void rules_argmax_kernel(ee_rules_call a, Rule
 
 // ---- launch shapes ----
 static const int kRulesPieces[] = {1024, 2048, 4096, 8192};
-// The longest piece of which the launch still has two workgroups per compute unit, up to 8192 tokens (a longer piece reads the history and meets its row less
-// often, but holds more of the table's LDS and of a compute unit's arithmetic: 144 rows of 128256 tokens 53 us, in pieces of 16384 62, of 4096 55, of 2048 82;
-// 96 whole rows of 32003 tokens 21 us, in pieces of 4096 19), or what covers the vocabulary.
+// The longest piece of which the launch still has two workgroups per compute unit, up to 8192 tokens, or what covers the vocabulary.  A longer piece reads the
+// history and meets its row less often, but holds more of the table's LDS and of a compute unit's arithmetic: 512 rows of 128256 tokens take
+// 127 us in pieces of 8192 (512 threads; with 256 threads 134) and 142 in pieces of 4096, 144 rows 49 (58) and 52, 64 greedy rows 27 (28) and 30.
 static int rules_piece(int rows, int vocab) {
   int piece = kRulesPieces[0];
   for (int c : kRulesPieces)
