@@ -459,7 +459,10 @@ extern "C" int ee_debug_rules_looks(int looks) {
   return EE_OK;
 }
 
-static const long kRulesMeet = 2L << 20;               // values of a call beyond which the pieces meet
+// Values of a call beyond which the pieces meet: below, a second pass over what lies in the caches is quicker than a launch that clears the words and the
+// wait.  Rows of 128256 tokens, meeting / second pass: 8 rows 16.1 / 13.0 us, 16 16.2 / 15.3, 24 16.2 / 18.2, 64 27.7 / 37.2, 256 82 / 112; of 32003: 32 rows
+// 16.2 / 13.1, 64 15.6 / 16.2, 128 16.1 / 21.7.
+static const long kRulesMeet = 2L << 20;
 void k_rules(hipStream_t st, const ee_rules_call& a, const RulesStep& step) {
   if (a.rows <= 0 || a.n_seq <= 0) return;
   const int piece = rules_piece(a.rows, a.vocab);
@@ -470,7 +473,6 @@ void k_rules(hipStream_t st, const ee_rules_call& a, const RulesStep& step) {
   wk.n_late = (unsigned*)a.workspace;
   wk.looks = g_rules_looks;
   const int words = wk.pieces * a.rows;
-  // A small softmax takes a second pass instead of the meeting (one row of 128256 tokens 13.7 us a call, meeting 18.6: a launch more)
   const bool joined = a.probs && wk.pieces > 1, meet = joined && (long)a.rows * a.vocab > kRulesMeet;
   if (joined && !meet) wk.looks = -1;
   if (meet) hipLaunchKernelGGL(rules_clear_kernel, dim3(ceil_div(words, 256)), dim3(256), 0, st, wk, words);
