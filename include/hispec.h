@@ -426,7 +426,7 @@ int ee_debug_attention_split_pages(int pages);
  * 2 a wave per page (1 and 2 unsplit; all three serve any call) -- or -1, the built-in choice.  EE_ERR_ARG for any other
  * value.  ee_debug_last_attention returns the one that the session's last pass took (-1 before the first and for fp32; 3: shared
  * pages once for all their sequences).  ee_debug_shared_attention, process-wide: 1 takes that form wherever sequences of a call share
- * pages, 0 never, -1 restores the built-in choice; a forced form or split length of the two calls above goes first. */
+ * pages (ee_attend: reads them together), 0 never, -1 restores the built-in choice; a forced form or split length of the two calls above goes first. */
 int ee_debug_attention_form(int form);
 int ee_debug_last_attention(const ee_session* s);
 int ee_debug_shared_attention(int mode);

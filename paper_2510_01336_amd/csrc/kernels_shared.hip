@@ -63,7 +63,8 @@ __device__ inline void store_stats(const SharedCall& a, int slot, int kvh, int q
 
 // An item of one or two tiles: latency, not arithmetic, bounds it, so its pages go straight to registers, a page per wave: four waves (two of each tile) take
 // every fourth (second) page, 128 KiB in flight a workgroup, no barrier before the waves of a tile meet in LDS at the end.  A round of four (two) pages takes
-// 1.4 to 1.7 us, four sequences of 540 positions 7.5 us a launch.
+// 1.4 to 1.7 us, 16 sequences of 500 positions 7.6 us a
+// call with one tile each and 10.1 with two (by the other form, through LDS with a barrier a page, 13.5 and 14.9), of 4000 positions 40 and 46 (75 and 48).
 struct SharedItemView { int tile0, n_tiles, page0, npg, slot0, kv_end, first_masked; bool own; table_t bt; };
 template <int D, bool ROWS>
 __device__ __forceinline__ void shared_narrow(const SharedCall& a, const SharedItemView& it, int kvh, u32x4* lds) {

@@ -486,12 +486,13 @@ static int share_attention(ee_session* s, int si, CallPlan& p, int steps, bool a
   // A run of one page is not worth a segment: 16 to 48 sequences behind 4096 shared positions, in groups that share one page more, take 0.1 to
   // 0.6 us longer with it than without; of 2 and 4 pages it is the same either way, of 8 the segment saves up to 6 us.
   const int least = 2;
-  SharedPlan P = plan_shared(q, rep, (int)s->part_units, wgs, least, true);
+  SharedPlan P = plan_shared(q, rep, (int)s->part_units, wgs, least, g_shared_attention != 0);
   SharedSlot& sl = s->shared[si];
   auto fits = [&](const SharedPlan& x) {
     return x.items.size() < 65536 && 8 * x.items.size() + 4 * x.rows.size() + 4 * x.joins.size() + x.entries.size() + 16 <= s->shared_cap && (size_t)x.slots <= s->part_units;
   };
-  if (always && P.shares && named <= 4 * wgs) {          // few pages: uncut and unshared a call needs no joining, one launch instead of two
+  // few pages: uncut and unshared a call needs no joining, one launch instead of two (four sequences of 540 positions 7.1 us, shared 8.5)
+  if (always && g_shared_attention < 0 && P.shares && named <= 4 * wgs) {
     SharedPlan one = plan_shared(q, rep, (int)s->part_units, wgs, least, false);
     if (fits(one) && one.us < P.us) P = std::move(one);
   }

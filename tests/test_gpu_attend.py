@@ -89,10 +89,12 @@ class Planted:
 
     def attend(self, rows, pos0=None, **kw):
         q = self.query(rows)
-        self.sess.attend_begin(rows, pos0)
         at = pos0 if pos0 is not None else [n - m for n, m in zip(self.lens, rows)]
-        got = self.sess.attend(self.layer, self.tensor(q), **kw)
-        self.check(q, rows, at, got)
+        for mode in (0, 1, -1):                                  # never together, together wherever pages are shared, the built-in choice
+            hs.ee_debug_shared_attention(mode)
+            self.sess.attend_begin(rows, pos0)
+            got = self.sess.attend(self.layer, self.tensor(q), **kw)
+            self.check(q, rows, at, got)
         return q, got
 
     def close(self):
@@ -185,13 +187,16 @@ def test_what_lies_behind_the_rows_does_not_matter():
     P.close()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_strides_streams_and_graphs(dtype):
+@pytest.mark.parametrize("dtype, mode", [("bf16", -1), ("bf16", 1), ("f32", -1)])
+def test_strides_streams_and_graphs(dtype, mode):
     cfg = config(8, 2, 64, dtype)
     P = Planted(cfg, {"p": 150, "a": 30, "b": 8, "c": 1}, [("p", "a"), ("p", "b"), ("p", "c")])
     rows = [3, 2, 1]
-    q, want = P.attend(rows)
+    q, _ = P.attend(rows)
     t = P.tensor(q)
+    hs.ee_debug_shared_attention(mode)
+    P.sess.attend_begin(rows)
+    want = P.sess.attend(1, t)
     # rows of a wider buffer, in and out; what lies between them stays
     wide = torch.full((6, 12, 64), 3.0, dtype=t.dtype, device="cuda")
     wide[:, 2:10] = t
@@ -214,8 +219,10 @@ def test_strides_streams_and_graphs(dtype):
     P.close()
     with torch.cuda.stream(side):
         P = Planted(cfg, {"p": 150, "a": 30, "b": 8, "c": 1}, [("p", "a"), ("p", "b"), ("p", "c")])
-        q, want = P.attend(rows)
+        q, _ = P.attend(rows)
         static = P.tensor(q)
+        hs.ee_debug_shared_attention(mode)
+        P.sess.attend_begin(rows)
         P.sess.attend(1, static)
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
