@@ -938,7 +938,10 @@ class LogitRules:
                 raise ValueError(f"{name}: one entry for each of {self.n_seq} sequences")
             setattr(c, name, t.data_ptr())
         if tokens is not None:
-            c.tokens_room, c.tokens_stride = tokens.shape[1], max(tokens.stride(0), tokens.shape[1])
+            room, stride = tokens.shape[1], tokens.stride(0)
+            if self.n_seq > 1 and stride < room:
+                raise ValueError("tokens: histories that do not overlap (an expanded tensor holds one for all)")
+            c.tokens_room, c.tokens_stride = room, max(stride, room)
         if allowed is not None:
             c.allowed_rows = allowed.shape[0]
             c.allowed_stride = allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]

@@ -266,6 +266,22 @@ def test_binding_refuses():
     assert out.shape == (0, 100) and tok.shape == (0,)
 
 
+def test_histories_that_overlap_are_refused():
+    """One history expanded over the sequences, or windows of one list, would be read from one room after another; of a single sequence any
+    stride is good."""
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    one, start, first = torch.full((40,), 7, dtype=torch.int32, device="cuda"), ints([0, 1, 2]), ints([40, 40])
+    rep = torch.full((2,), 2.0, device="cuda")
+    for tokens in (one[None].expand(2, 40), one.unfold(0, 20, 20 // 2)[:2]):
+        with pytest.raises(ValueError):
+            hs.LogitRules(100, start, tokens=tokens, first_len=first, repetition=rep)
+    x = torch.ones(1, 100, device="cuda")
+    got = hs.LogitRules(100, ints([0, 1]), tokens=one[None].expand(1, 40), first_len=first[:1], repetition=rep[:1]).logits(x)
+    want = x.clone()
+    want[0, 7] = 0.5
+    assert torch.equal(got, want)
+
+
 # ---- the rules of a session ------------------------------------------------------------------------------------------
 
 RULES = [dict(repetition=1.3, frequency=0.4, presence=0.5), dict(temperature=0.8, bias={5: 2.0, 17: -3.0, 900: 1.0}, repetition=0.9),
