@@ -154,6 +154,24 @@ def test_long_contexts_are_split_and_many_sequences():
     P.close()
 
 
+def test_offsets_behind_32_bits():
+    """A page pool whose last layer lies more than 2^32 elements into the cache; a copied page keeps every layer's contents."""
+    P = Planted(config(32, 8, 128), {"p": 300, "a": 20, "b": 90}, [("p", "a"), ("p", "b")], layer=2, pages=20000)
+    assert 2 * 20000 * 8 * 2 * PAGE * 128 > 2 ** 32
+    P.attend([1, 1])
+    P.attend([9, 3])
+    before = [P.sess.read_kv(1, l, 0, 200) for l in range(3)]
+    P.sess.rollback(1, 0b111, 200)
+    P.sess.decode_ar(1)                                         # position 200 on is written: the shared page is copied
+    assert P.sess.shared_pages(1) == 3
+    for l, want in enumerate(before):
+        for x, y in zip(P.sess.read_kv(1, l, 0, 200), want):
+            assert np.array_equal(x, y), l
+    for x, y in zip(P.sess.read_kv(0, 2, 0, 300), (P.K[0], P.V[0])):
+        assert np.array_equal(np.asarray(x).reshape(-1), y[:300].reshape(-1))
+    P.close()
+
+
 def test_nothing_shared_and_one_sequence():
     runs = {"a": 100, "b": 700, "c": 5}
     P = Planted(config(32, 8, 128), runs, [("a",), ("b",), ("c",)])
